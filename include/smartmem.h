@@ -433,6 +433,93 @@ size_t sm_decode_step_workspace_bytes(const sm_decode_cfg*, int mode);
 int sm_decode_step(const sm_decode_cfg*, const sm_decode_weights*, const void* x, void* k_cache, void* v_cache,
                    void* y, void* k_out, void* v_out, void* ws, size_t ws_bytes, int mode, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* A paged key / value cache: requests of ragged lengths                      */
+/* ------------------------------------------------------------------------ */
+
+/* sm_decode_step keeps one contiguous cache for sequences of one length.  A server whose requests differ in length keeps
+ * the keys and values of a layer in a pool of n_pages pages of `page` tokens instead; row r of a page table names the
+ * pages of request r, token position p lies in page table[r][p / page] at place p % page, and that page's id times `page`
+ * plus p % page is the token's slot.  The operators below follow the rule of Sec. 3.2.2 with a map that only the device
+ * knows: the producer of a key stores it where the attention reads it, and no gather or append copies the cache.
+ * Tables, lengths, positions and slots are int32 device arrays, so that a captured graph can be replayed on new ones;
+ * what a kernel reads from them is checked against the bounds the host passed (an entry outside them stands for "no such
+ * page" / "no such slot" and is neither read nor written through).  A tensor may be any strided view with a contiguous
+ * last axis: base address and strides (in elements) keep 16-byte alignment. */
+
+/* Page table and slot map of an iteration: request r has cached[r] tokens in its pages and brings fresh[r] new ones
+ * (0 allowed; negative counts as 0).  One kernel; nothing is read back.
+ *   row length: max_pages * page tokens; c = min(cached[r], row length)
+ *   starts [n_req + 1]: first token row of every request, sum of fresh before it, at most max_tokens (later tokens have no row)
+ *   positions [max_tokens]: c + j for the j-th new token of a request; -1 from starts[n_req] on (padding)
+ *   table [n_req rows of table_pitch >= max_pages]: pages that the new tokens open are taken from free_pages (device
+ *     [free_cap], the first *n_free valid, device) in the order of the requests and written behind the ones the row has;
+ *     no other entry is touched
+ *   slots [max_tokens]: see above; -1 for padding, for tokens behind the end of the row, for tokens whose page could not
+ *     be had because free_pages ran out, and where the page id lies outside [0, n_pages)
+ *   lens [n_req]: tokens that the request's pages hold after the iteration: c + fresh[r], less what found no row or page
+ *   need [1]: pages the call wanted; free_pages ran out if it exceeds *n_free.  The first min(*need, *n_free) are taken.
+ * The outputs must not overlap the inputs (except `table`, which is both).  The same call again gives the same result.
+ * Limits: n_req <= 65536, max_tokens, n_req * max_pages, n_pages * page and max_pages * page <= 2^30. */
+typedef struct { int32_t n_req, page, max_pages, n_pages, free_cap, max_tokens; int64_t table_pitch; } sm_page_cfg;
+int sm_page_table(const sm_page_cfg*, const int32_t* cached, const int32_t* fresh, const int32_t* free_pages, const int32_t* n_free,
+                  int32_t* table, int32_t* starts, int32_t* lens, int32_t* positions, int32_t* slots, int32_t* need, void* stream);
+
+/* Norm of every query and key head, rotary embedding and the store into the cache, in one pass over the projection:
+ *   n = LayerNorm(x) / RMSNorm(x) / x over the d features of a head (norm as in sm_linear_desc: 1 / 2 / 0; gamma [d],
+ *       beta [d] for LayerNorm, shared by the heads of q resp. k), then features [0, rot) rotated in half-split pairs
+ *       (i, i + rot/2) by the angle positions[t] * rope_base^(-2i/rot); the rest as normalised.  fp32 until the store.
+ * q [tokens, heads_q, d] -> q_out; k [tokens, heads_kv, d] -> k_out; v -> v_out unchanged.  q, k, v may each be null
+ * (with its output): that part is left out.  Strides: token, head for inputs and q_out; page, token, head for k_out and
+ * v_out.  slots null: row t of k_out / v_out is t * stride[1] + head * stride[2].  slots given: k_out / v_out are page
+ * pools and row t goes to page slots[t] / page, place slots[t] % page; a slot outside [0, n_pages * page) stores nothing.
+ * A token with a negative position is padding: nothing of it is read or written.  Two tokens of one slot: each head of
+ * the slot holds either of them.  An output may be its input (same address and strides), otherwise they must not overlap.
+ * Angles are exact to a 2^-31 revolution at any position.  rot a multiple of twice the 16-byte vector (16 bf16, 8 f32),
+ * d a multiple of the vector, both at most 256; rope_base >= 1; n_pages * page <= 2^30. */
+typedef struct {
+  int32_t dtype, tokens, heads_q, heads_kv, d;
+  int32_t norm; float eps;
+  const void *q_gamma, *q_beta, *k_gamma, *k_beta;
+  int32_t rot; float rope_base;
+  int32_t page, n_pages;                                                    /* with slots only */
+  int64_t q_stride[2], k_stride[2], v_stride[2], q_out_stride[2], k_out_stride[3], v_out_stride[3];
+} sm_head_norm_rope_desc;
+int sm_head_norm_rope(const sm_head_norm_rope_desc*, const void* q, const void* k, const void* v, const int32_t* positions,
+                      const int32_t* slots, void* q_out, void* k_out, void* v_out, void* stream);
+
+/* Attention of one new token per request over its pages:  o[r, h] = softmax(scale * q[r, h] . K^T) V over the
+ * min(lens[r], max_pages * page) first tokens of request r, head h reading key head h / (heads_q / heads_kv) (heads_q a
+ * multiple of heads_kv).  No token (lens[r] <= 0, or no page of them exists): o = 0, lse = -inf.  lse (nullable)
+ * [n_req, heads_q] fp32, contiguous: the natural logarithm of the sum of exp(scale * q . k), with which results over
+ * disjoint parts of a cache can be joined.  What lies in a page behind the request's last token is not used, whatever
+ * it is.  Strides: request, head (q, o); page, token, head (k_pages, v_pages: token-major [page, token, head, d] and
+ * head-major [page, head, token, d] pools alike).  The key axis is split over workgroups by the lengths found on the
+ * device and joined in fp32.
+ * d a multiple of the 16-byte vector (8 bf16, 4 f32), at most 256.  The workspace holds partial results; nothing in it
+ * has to survive between calls; calls that share one on different streams race. */
+typedef struct {
+  int32_t dtype, n_req, heads_q, heads_kv, d, page, max_pages, n_pages;
+  float scale;
+  int64_t table_pitch, q_stride[2], o_stride[2], k_stride[3], v_stride[3];
+} sm_paged_attention_desc;
+size_t sm_paged_attention_workspace_bytes(const sm_paged_attention_desc*);
+int sm_paged_attention(const sm_paged_attention_desc*, const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
+                       const int32_t* lens, void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Linear on few rows with weights of 4 bits:  y = act(x W^T + bias) + residual,  W[n, k] = (w[n, k] - z[n, k / group]) *
+ * s[n, k / group].  x [M, K], y and residual [M, N], bias [N], s [N, K / group] bf16; w [N, K / 2] bytes, the even k in the
+ * low four bits; z [N, K / group] bytes 0 .. 15, null: 8 throughout.  group 32, 64 or 128; K a multiple of it; act
+ * SM_ACT_NONE or SM_ACT_GELU (erf).  sm_linear_w4_pack writes weights, scales and zero points into `packed`
+ * (sm_linear_w4_packed_bytes, caller-owned device memory) in the order the kernel reads them, once.  The products are
+ * exact (integers times bf16, fp32 sums); a group's sum takes its scale in fp32.  Made for the rows of a decode step: the
+ * weights are streamed once per 32 rows. */
+typedef struct { int32_t M, N, K, group, act; } sm_linear_w4_desc;
+size_t sm_linear_w4_packed_bytes(int N, int K, int group);
+int sm_linear_w4_pack(const void* w, const void* scales, const void* zeros, int N, int K, int group, void* packed, void* stream);
+int sm_linear_w4(const sm_linear_w4_desc*, const void* x, const void* packed, const void* bias, const void* residual, void* y,
+                 void* stream);
+
 /* Cross-shaped window self-attention of the CSwin Transformer (Table 1 counts its
  * Reshape / Transpose operators, Table 7 evaluates it): the stripe partition,
  * head split, head merge and stripe merge around the two attentions are Reshape /

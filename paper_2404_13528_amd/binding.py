@@ -5,6 +5,7 @@ host-side planner and index-map composer, its C++ host code).  There is no
 Python or CPU fallback: if the library is missing, loading raises.
 torch is used for device memory and streams only.
 """
+import collections
 import ctypes as C
 import os
 
@@ -130,7 +131,8 @@ def lib():
         L.sm_map_numel.restype = C.c_int64
         for f in ("sm_fanout_graph_workspace_bytes", "sm_swin_block_workspace_bytes", "sm_attn_block_workspace_bytes", "sm_run_chain_workspace_bytes",
                   "sm_swin_block_static_max_bytes", "sm_decode_step_workspace_bytes",
-                  "sm_cswin_attention_workspace_bytes", "sm_cswin_block_workspace_bytes"):
+                  "sm_cswin_attention_workspace_bytes", "sm_cswin_block_workspace_bytes", "sm_paged_attention_workspace_bytes",
+                  "sm_linear_w4_packed_bytes"):
             getattr(L, f).restype = C.c_size_t
         _lib = L
     return _lib
@@ -769,6 +771,207 @@ class DecodeStep:
                                    _ptr(vo), _ptr(self.ws), C.c_size_t(self.ws.numel()), self.mode, _stream(stream)),
               "sm_decode_step")
         return (y, ko, vo) if self.mode == SM_EXPLICIT else y
+
+
+# --------------------------------------------------------------------------
+# a paged key / value cache and the Linears around it
+# --------------------------------------------------------------------------
+
+def _take(t, name, dtype, shape=None, device=None, rows=False):
+    """Checks a device tensor before its address goes to the library: dtype, shape (None: any extent), one device, and a
+    contiguous last axis (rows=True) or contiguous throughout."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a tensor on the GPU" % name)
+    if t.device.index != torch.cuda.current_device() or (device is not None and t.device != device):
+        raise ValueError("%s is on %s: all tensors of a call belong to the current device" % (name, t.device))
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if shape is not None and (t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape))):
+        raise ValueError("%s must have the shape %s, not %s" % (name, tuple("any" if w is None else w for w in shape), tuple(t.shape)))
+    if rows:
+        if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("the last axis of %s must be contiguous" % name)
+    elif not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t
+
+
+class PageCfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_req", "page", "max_pages", "n_pages", "free_cap", "max_tokens")] + [("table_pitch", C.c_int64)]
+
+
+PageTable = collections.namedtuple("PageTable", "starts lens positions slots need")
+
+
+def page_table(cached, fresh, free_pages, n_free, table, page, n_pages, max_tokens, out=None, stream=None):
+    """sm_page_table: pages and slots of the new tokens of an iteration, from lengths on the device.  cached, fresh [R], free_pages,
+    n_free [1] and table [R, max_pages] (updated in place) are int32 device tensors.  Returns PageTable(starts [R + 1], lens [R],
+    positions [max_tokens], slots [max_tokens], need [1]), or fills the one given as `out`."""
+    import torch
+    i32 = torch.int32
+    R = _take(cached, "cached", i32, (None,)).shape[0]
+    _take(fresh, "fresh", i32, (R,))
+    _take(free_pages, "free_pages", i32, (None,))
+    _take(n_free, "n_free", i32, (1,))
+    _take(table, "table", i32, (R, None), rows=True)
+    max_tokens = int(max_tokens)
+    shapes = {"starts": R + 1, "lens": R, "positions": max_tokens, "slots": max_tokens, "need": 1}
+    if out is None:
+        out = PageTable(*[torch.empty(max(0, n), dtype=i32, device=cached.device) for n in shapes.values()])
+    for name, n in shapes.items():
+        _take(getattr(out, name), name, i32, (n,))
+    cfg = PageCfg(R, int(page), table.shape[1], int(n_pages), free_pages.shape[0], max_tokens, table.stride(0) if R > 1 else table.shape[1])
+    check(lib().sm_page_table(C.byref(cfg), _ptr(cached), _ptr(fresh), _ptr(free_pages), _ptr(n_free), _ptr(table), _ptr(out.starts),
+                              _ptr(out.lens), _ptr(out.positions), _ptr(out.slots), _ptr(out.need), _stream(stream)), "sm_page_table")
+    return out
+
+
+class HeadNormRopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "tokens", "heads_q", "heads_kv", "d", "norm")] + [("eps", C.c_float)] + \
+               [(n, C.c_void_p) for n in ("q_gamma", "q_beta", "k_gamma", "k_beta")] + [("rot", C.c_int32), ("rope_base", C.c_float)] + \
+               [(n, C.c_int32) for n in ("page", "n_pages")] + [(n, C.c_int64 * 2) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride")] + \
+               [(n, C.c_int64 * 3) for n in ("k_out_stride", "v_out_stride")]
+
+
+HEAD_NORM = {"none": 0, "layer": 1, "rms": 2}
+
+
+def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gamma=None, q_beta=None, k_beta=None, rot=None,
+                   rope_base=10000.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
+    """sm_head_norm_rope.  q [T, heads_q, d], k and v [T, heads_kv, d] (strided views; each may be None), positions [T] int32 (negative:
+    padding).  norm "rms" / "layer" / "none" over d; rot: rotated features (None: all d).  slots [T] int32: k and v go to their slots
+    of the pools k_out / v_out [n_pages, page, heads_kv, d] (strided views, so a head-major pool is passed permuted); without slots
+    k_out / v_out are [T, heads_kv, d] (new tensors by default), as q_out always is.  Returns (q_out, k_out, v_out)."""
+    import torch
+    first = next((t for t in (q, k, v) if t is not None), None)
+    if first is None:
+        raise ValueError("q, k and v are all None")
+    if first.dim() != 3:
+        raise ValueError("q, k and v have three axes: token, head, feature")
+    dt, dev, (T, _, d) = first.dtype, first.device, first.shape
+    desc = HeadNormRopeDesc()
+    desc.dtype, desc.tokens, desc.d, desc.norm, desc.eps = _dt(first), T, d, HEAD_NORM[norm], eps
+    desc.rot, desc.rope_base = d if rot is None else int(rot), rope_base
+    _take(positions, "positions", torch.int32, (T,), dev)
+    if slots is not None:
+        _take(slots, "slots", torch.int32, (T,), dev)
+        pool = k_out if k is not None else v_out
+        if pool is None or pool.dim() != 4:
+            raise ValueError("slots need the page pools k_out / v_out [n_pages, page, heads_kv, d]")
+        desc.n_pages, desc.page = pool.shape[:2]
+    kv = next((t for t in (k, v) if t is not None), None)
+    desc.heads_kv = 0 if kv is None else kv.shape[1]
+    desc.heads_q = 0 if q is None else q.shape[1]
+    outs = []
+    for n, x, y, heads in (("q", q, q_out, desc.heads_q), ("k", k, k_out, desc.heads_kv), ("v", v, v_out, desc.heads_kv)):
+        if x is None:
+            outs.append(None)
+            continue
+        _take(x, n, dt, (T, heads, d), dev, rows=True)
+        paged = slots is not None and n != "q"
+        if y is None and not paged:
+            y = torch.empty((T, heads, d), dtype=dt, device=dev)
+        _take(y, n + "_out", dt, (desc.n_pages, desc.page, heads, d) if paged else (T, heads, d), dev, rows=True)
+        outs.append(y)
+        for i in range(2):
+            getattr(desc, n + "_stride")[i] = x.stride(i)
+        st = [s for s in y.stride()[:-1]]
+        for i, s in enumerate(st if n == "q" or paged else [0] + st):
+            getattr(desc, n + "_out_stride")[i] = s
+        if n != "v":
+            for part, g in (("gamma", q_gamma if n == "q" else k_gamma), ("beta", q_beta if n == "q" else k_beta)):
+                if g is not None:
+                    _take(g, "%s_%s" % (n, part), dt, (d,), dev)
+                setattr(desc, "%s_%s" % (n, part), _ptr(g).value)
+    check(lib().sm_head_norm_rope(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(slots), _ptr(outs[0]), _ptr(outs[1]),
+                                  _ptr(outs[2]), _stream(stream)), "sm_head_norm_rope")
+    return tuple(outs)
+
+
+class PagedAttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "n_req", "heads_q", "heads_kv", "d", "page", "max_pages", "n_pages")] + [("scale", C.c_float)] + \
+               [("table_pitch", C.c_int64)] + [(n, C.c_int64 * 2) for n in ("q_stride", "o_stride")] + [(n, C.c_int64 * 3) for n in ("k_stride", "v_stride")]
+
+
+class PagedAttention:
+    """sm_paged_attention; owns its workspace.  q [n_req, heads_q, d], k_pages / v_pages [n_pages, page, heads_kv, d] (strided views: a
+    head-major pool is passed permuted), table [n_req, max_pages] and lens [n_req] int32 -> o [n_req, heads_q, d]; lse: a contiguous
+    fp32 [n_req, heads_q] to fill with the logarithm of the softmax sums.  Calls of one object on different streams race."""
+
+    def __init__(self, n_req, heads_q, heads_kv, d, page, max_pages, n_pages, dtype, scale=None):
+        import torch
+        c = PagedAttentionDesc()
+        c.dtype = SM_F32 if dtype == torch.float32 else SM_BF16
+        c.n_req, c.heads_q, c.heads_kv, c.d, c.page, c.max_pages, c.n_pages = n_req, heads_q, heads_kv, d, page, max_pages, n_pages
+        c.scale = d ** -0.5 if scale is None else scale
+        c.table_pitch = max_pages
+        self.desc, self.dtype = c, dtype
+        n = lib().sm_paged_attention_workspace_bytes(C.byref(c))
+        if n == 0:
+            raise SmError("sm_paged_attention_workspace_bytes: " + lib().sm_last_error().decode())
+        self.ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+
+    def __call__(self, q, k_pages, v_pages, table, lens, out=None, lse=None, stream=None):
+        import torch
+        c, dt, dev = self.desc, self.dtype, self.ws.device
+        _take(q, "q", dt, (c.n_req, c.heads_q, c.d), dev, rows=True)
+        for n, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+            _take(t, n, dt, (c.n_pages, c.page, c.heads_kv, c.d), dev, rows=True)
+        _take(table, "table", torch.int32, (c.n_req, c.max_pages), dev, rows=True)
+        _take(lens, "lens", torch.int32, (c.n_req,), dev)
+        if out is None:
+            out = torch.empty((c.n_req, c.heads_q, c.d), dtype=dt, device=dev)
+        _take(out, "out", dt, (c.n_req, c.heads_q, c.d), dev, rows=True)
+        if lse is not None:
+            _take(lse, "lse", torch.float32, (c.n_req, c.heads_q), dev)
+        d = PagedAttentionDesc.from_buffer_copy(c)
+        d.table_pitch = table.stride(0) if c.n_req > 1 else c.max_pages
+        for i in range(2):
+            d.q_stride[i], d.o_stride[i] = q.stride(i), out.stride(i)
+        for i in range(3):
+            d.k_stride[i], d.v_stride[i] = k_pages.stride(i), v_pages.stride(i)
+        check(lib().sm_paged_attention(C.byref(d), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), _ptr(lens), _ptr(out), _ptr(lse),
+                                       _ptr(self.ws), C.c_size_t(self.ws.numel()), _stream(stream)), "sm_paged_attention")
+        return out
+
+
+class LinearW4Desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("M", "N", "K", "group", "act")]
+
+
+class LinearW4:
+    """sm_linear_w4: a Linear whose weights stay in 4 bits.  w [N, K / 2] uint8 (even k in the low four bits), scales [N, K / group]
+    bf16, zeros [N, K / group] uint8 (None: 8), bias [N] bf16 or None.  The weights are packed here, once, into memory of the
+    object (a change of them afterwards needs a new object)."""
+
+    def __init__(self, w, scales, zeros=None, group=128, bias=None, stream=None):
+        import torch
+        N, K = _take(w, "w", torch.uint8, (None, None)).shape[0], 2 * w.shape[1]
+        n = lib().sm_linear_w4_packed_bytes(N, K, int(group))
+        if n == 0:
+            raise SmError("sm_linear_w4_packed_bytes: " + lib().sm_last_error().decode())
+        _take(scales, "scales", torch.bfloat16, (N, K // group), w.device)
+        if zeros is not None:
+            _take(zeros, "zeros", torch.uint8, (N, K // group), w.device)
+        if bias is not None:
+            _take(bias, "bias", torch.bfloat16, (N,), w.device)
+        self.N, self.K, self.group, self.bias = N, K, int(group), bias
+        self.packed = torch.empty(n, dtype=torch.uint8, device=w.device)
+        check(lib().sm_linear_w4_pack(_ptr(w), _ptr(scales), _ptr(zeros), N, K, self.group, _ptr(self.packed), _stream(stream)), "sm_linear_w4_pack")
+
+    def __call__(self, x, residual=None, act="none", out=None, stream=None):
+        import torch
+        bf16, dev = torch.bfloat16, self.packed.device
+        M = _take(x, "x", bf16, (None, self.K), dev).shape[0]
+        if residual is not None:
+            _take(residual, "residual", bf16, (M, self.N), dev)
+        if out is None:
+            out = torch.empty((M, self.N), dtype=bf16, device=dev)
+        _take(out, "out", bf16, (M, self.N), dev)
+        d = LinearW4Desc(M, self.N, self.K, self.group, ACT[act])
+        check(lib().sm_linear_w4(C.byref(d), _ptr(x), _ptr(self.packed), _ptr(self.bias), _ptr(residual), _ptr(out), _stream(stream)), "sm_linear_w4")
+        return out
 
 
 class CswinAttention:

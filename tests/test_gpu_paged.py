@@ -1,0 +1,467 @@
+"""The operators over a paged key / value cache against oracle/paged.py: page table and slots (equal), per-head norm + rotation +
+store, attention of one new token, and a decode iteration that runs them together.
+
+Tolerances, per element.  A store rounds by half a step: bf16 2^-8, fp32 2^-24 of the value.
+Norm and rotation: the sums of d <= 256 squares are added as trees over the lanes (at most 8 + 6 additions deep), the square root, the
+division and the products add a few roundings more, and mean and square root see x's own size: 40 * 2^-24 of the largest value that
+occurs on the way.  The angle's rounding to fp32 (2^-25 of a revolution) and a sine of 2^-20 absolute in bf16 (the hardware's), 2^-22 in
+fp32 (the library's), times the pair.
+Attention: a logit's error is below (d + 4) 2^-24 of sum |q k| * |scale| (products exact in bf16, sums in fp32), and moves a weight by
+that much, numerator and denominator; the weights themselves carry 2^-16 (bf16: two terms of 8 bits each) resp. 2^-22, and sums of up
+to n keys in blocks (n / 16 + 64) 2^-24 of sum p |v|."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops as O, paged as P
+from paper_2404_13528_amd import binding as sm
+from util import to_np
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+HALF = {BF16: 2.0 ** -8, F32: 2.0 ** -24}
+I32 = torch.int32
+
+
+def ints(x, pad=None):
+    return torch.tensor(x, dtype=I32).cuda()
+
+
+def check(got, want, tol, what):
+    got = to_np(got)
+    assert got.shape == want.shape, (what, got.shape, want.shape)
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), "%s: %d of %d off, first at %s: %r for %r, tolerance %r" % (
+        what, bad.sum(), bad.size, np.argwhere(bad)[0], got[bad][0], want[bad][0], np.broadcast_to(tol, bad.shape)[bad][0])
+
+
+# ------------------------------------------------------------------------------------------------ page table
+
+def page_case(cached, fresh, page, cols, spare=5, short=0, pad=0, pitch=0, seed=0):
+    """Runs sm_page_table and the oracle; the table's pitch may be larger than its row."""
+    rng = np.random.default_rng(seed)
+    R, row = len(cached), cols * page
+    held = [-(-min(max(c, 0), row) // page) for c in cached]
+    ends = [min(min(max(c, 0), row) + max(f, 0), row) for c, f in zip(cached, fresh)]
+    new = sum(-(-e // page) - h for e, h in zip(ends, held))
+    n_pages = sum(held) + new + spare
+    ids = rng.permutation(n_pages)
+    table = np.full((R, cols + pitch), -7)
+    at = 0
+    for r in range(R):
+        table[r, :held[r]] = ids[at:at + held[r]]
+        at += held[r]
+    free = ids[at:]
+    n_free = max(0, new - short) if short else len(free)
+    T = max(0, sum(max(f, 0) for f in fresh) + pad)
+    want = P.page_table(cached, fresh, free, n_free, table[:, :cols], page, n_pages, T)
+    td = ints(table)
+    out = sm.page_table(ints(cached), ints(fresh), ints(free), ints([n_free]), td[:, :cols], page, n_pages, T)
+    for _ in range(2):                                 # the same call again: the same result
+        torch.cuda.synchronize()
+        got = td.cpu().numpy()
+        assert (got[:, :cols] == want[0]).all() and (got[:, cols:] == -7).all()
+        for g, w, n in zip(out, want[1:5], out._fields):
+            assert (g.cpu().numpy() == w).all(), (n, g.cpu().numpy(), w)
+        assert out.need.item() == want[5]
+        sm.page_table(ints(cached), ints(fresh), ints(free), ints([n_free]), td[:, :cols], page, n_pages, T, out=out)
+
+
+@pytest.mark.parametrize("cached,fresh,page,cols", [
+    ([0], [0], 1, 1), ([0], [1], 16, 1), ([15], [1], 16, 2), ([16], [1], 16, 2), ([17], [0], 16, 2), ([3, 4, 0], [2, 0, 5], 4, 3),
+    ([0, 0, 0, 0], [0, 0, 0, 0], 8, 2), ([-5, 7, 3], [4, -9, 30], 8, 3),        # negative counts, a row that ends
+    ([100, 0], [5, 40], 8, 4),                                                   # more cached than the row holds
+    ([0, 31], [2500, 1], 32, 100), ([5], [5000], 1, 5005), ([7, 9], [1030, 2], 3, 400)])
+def test_page_table_small(cached, fresh, page, cols):
+    for pad, short, pitch in ((0, 0, 0), (3, 1, 2), (-1, 0, 1), (1500, 2, 0)):
+        page_case(cached, fresh, page, cols, pad=pad, short=short, pitch=pitch)
+
+
+@pytest.mark.parametrize("R", [1, 63, 64, 65, 255, 256, 257, 511, 1000, 2049])
+def test_page_table_many_requests(R):
+    rng = np.random.default_rng(R)
+    cached = rng.integers(0, 50, R).tolist()
+    page_case(cached, [1] * R, 16, 5, seed=R)
+    page_case(cached, rng.integers(0, 40, R).tolist(), 8, 12, pad=100, short=R // 2, seed=R)
+    page_case(cached, (rng.integers(0, 30, R) * (rng.random(R) < 0.1)).tolist(), 4, 20, pad=-int(R // 3), seed=R)
+
+
+def test_page_table_without_tokens_or_free_pages():
+    e = torch.empty(0, dtype=I32, device="cuda")
+    t = ints([[3, -1]])
+    out = sm.page_table(ints([5]), ints([4]), e, ints([9]), t, 8, 4, 0)        # no rows: the new tokens are not there
+    assert out.lens.tolist() == [5] and out.starts.tolist() == [0, 0] and out.need.item() == 0
+    out = sm.page_table(ints([5]), ints([4]), e, ints([9]), t, 8, 4, 4)        # no page to take, whatever n_free says
+    assert out.lens.tolist() == [8] and out.slots.tolist() == [29, 30, 31, -1] and out.need.item() == 1 and t.tolist() == [[3, -1]]
+
+
+def test_page_table_bad_pages_have_no_slot():
+    out = sm.page_table(ints([1, 1, 0]), ints([1, 1, 2]), ints([99, 2]), ints([2]), ints([[-3], [64], [5]]), 16, 64, 4)
+    assert out.slots.tolist() == [-1, -1, -1, -1] and out.lens.tolist() == [2, 2, 2]
+
+
+# ------------------------------------------------------------------------------------------------ norm + rotation + store
+
+def head_norm_case(T, hq, hkv, d, rot, norm, dtype, paged=True, seed=0, page=16, base=10000.0, far=0, head_major=False, mean=0.0):
+    g = torch.Generator().manual_seed(seed)
+    qkv = (torch.randn(T, hq + 2 * hkv + 1, d, generator=g) + mean).to(dtype)          # (one head more: rows with a gap)
+    gam = {n: (1 + 0.2 * torch.randn(d, generator=g)).to(dtype) for n in ("q_gamma", "k_gamma")} if norm != "none" else {}
+    bet = {n: (0.5 * torch.randn(d, generator=g)).to(dtype) for n in ("q_beta", "k_beta")} if norm == "layer" else {}
+    pos = torch.randint(0, 3000, (T,), generator=g) + far
+    n_pages = -(-T // page) + 2
+    slots = torch.randperm(n_pages * page, generator=g)[:T]
+    if T > 3:
+        pos[2], slots[3] = -1, -1
+        slots[1] = n_pages * page                                                     # just behind the pool
+    fill = 77.0
+    shape = (n_pages, hkv, page, d) if head_major else (n_pages, page, hkv, d)
+    kp, vp = (torch.full(shape, fill, dtype=dtype, device="cuda") for _ in range(2))
+    x = qkv.cuda()
+    q, k, v = x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:hq + 2 * hkv]
+    q_out = torch.full((T, hq, d), fill, dtype=dtype, device="cuda")
+    kw = dict(norm=norm, rot=rot, rope_base=base, q_out=q_out, **{n: t.cuda() for n, t in {**gam, **bet}.items()})
+    view = (lambda t: t.permute(0, 2, 1, 3)) if head_major else (lambda t: t)
+    if paged:
+        sm.head_norm_rope(q, k, v, pos.to(I32).cuda(), slots=slots.to(I32).cuda(), k_out=view(kp), v_out=view(vp), **kw)
+        ko, vo = view(kp), view(vp)
+    else:
+        ko, vo = (torch.full((T, hkv, d), fill, dtype=dtype, device="cuda") for _ in range(2))
+        sm.head_norm_rope(q, k, v, pos.to(I32).cuda(), k_out=ko, v_out=vo, **kw)
+    torch.cuda.synchronize()
+    xn = to_np(qkv)
+    live = pos.numpy() >= 0
+    for n, part, got in (("q", xn[:, :hq], q_out), ("k", xn[:, hq:hq + hkv], ko)):
+        gamma, beta = (to_np(kw[n + s]) if n + s in kw else None for s in ("_gamma", "_beta"))
+        normed = P.head_norm(part, norm, gamma, beta, 1e-5)
+        want = P.rope(normed, pos.numpy(), rot, base)
+        # the largest value on the way: x itself (before the mean is taken off) and the shift
+        r = 1.0 if norm == "none" else np.abs(gamma).max() / np.sqrt(part.var(-1, keepdims=True) if norm == "layer" else (part ** 2).mean(-1, keepdims=True))
+        big = np.abs(part).max(-1, keepdims=True) * r + (np.abs(beta).max() if beta is not None else 0)
+        pair = np.abs(normed).max(-1, keepdims=True) * 2 * (2.0 ** -20 + 2 * np.pi * 2.0 ** -25 if dtype == BF16 else 2.0 ** -22 + 2 * np.pi * 2.0 ** -25)
+        tol = HALF[dtype] * np.abs(want) + 40 * 2.0 ** -24 * big + (pair if rot else 0)
+        if n == "q" or not paged:
+            full, ft = np.full(got.shape, fill), np.zeros(got.shape)
+            full[live], ft[live] = want[live], tol[live]
+            check(got, full, ft, n)
+        else:
+            full, ft = np.full((n_pages * page, hkv, d), fill), np.zeros((n_pages * page, hkv, d))
+            ok = live & (slots.numpy() >= 0) & (slots.numpy() < n_pages * page)
+            full[slots.numpy()[ok]], ft[slots.numpy()[ok]] = want[ok], tol[ok]
+            check(got, full.reshape(n_pages, page, hkv, d), ft.reshape(n_pages, page, hkv, d), n)
+    vw = xn[:, hq + hkv:hq + 2 * hkv]
+    if paged:
+        full = np.full((n_pages * page, hkv, d), fill)
+        full[slots.numpy()[ok]] = vw[ok]
+        assert (to_np(vo).reshape(-1, hkv, d) == full).all()
+    else:
+        full = np.full((T, hkv, d), fill)
+        full[live] = vw[live]
+        assert (to_np(vo) == full).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("norm", ["rms", "layer", "none"])
+@pytest.mark.parametrize("T,hq,hkv,d,rot", [(1, 1, 1, 64, 64), (5, 8, 2, 128, 128), (3, 3, 1, 96, 96), (7, 5, 5, 80, 32), (4, 2, 1, 256, 64),
+                                            (6, 4, 4, 256, 256), (2, 7, 1, 16, 16), (33, 2, 2, 72, 16), (130, 12, 4, 64, 0)])
+def test_head_norm_rope(T, hq, hkv, d, rot, norm, dtype):
+    head_norm_case(T, hq, hkv, d, rot, norm, dtype, seed=T + d, head_major=T % 2 == 0, page=1 + T % 16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_head_norm_rope_plain_rows_and_far_positions(dtype):
+    head_norm_case(9, 6, 2, 128, 128, "rms", dtype, paged=False)
+    head_norm_case(9, 6, 2, 64, 64, "none", dtype, paged=False, far=2 ** 31 - 3001)
+    head_norm_case(700, 4, 1, 128, 64, "rms", dtype, far=1000000, base=5e5, page=64)
+    head_norm_case(5, 4, 1, 64, 64, "layer", dtype, mean=30.0)                      # a mean that has to be taken off before squaring
+    head_norm_case(1500, 2, 1, 128, 128, "rms", dtype, page=8)
+
+
+def test_head_norm_rope_parts_in_place_and_empty():
+    x = torch.randn(6, 4, 64, device="cuda")
+    g = torch.ones(64, device="cuda")
+    pos = torch.arange(6, dtype=I32, device="cuda")
+    q, _, _ = sm.head_norm_rope(x, None, None, pos, q_gamma=g)
+    _, k, _ = sm.head_norm_rope(None, x, None, pos, k_gamma=g)
+    assert torch.equal(q, k)
+    _, _, v = sm.head_norm_rope(None, None, x, pos)
+    assert torch.equal(v, x)
+    y = x.clone()
+    sm.head_norm_rope(y, None, None, pos, q_gamma=g, q_out=y)
+    assert torch.equal(y, q)
+    out = sm.head_norm_rope(x[:0], x[:0], x[:0], pos[:0], q_gamma=g, k_gamma=g)
+    assert [t.shape[0] for t in out] == [0, 0, 0]
+    # zeros: the norm of a zero head is zero (eps), infinities and NaN stay in their head
+    z = torch.zeros(2, 2, 64, device="cuda")
+    z[0, 1, 3], z[1, 0, 5] = float("inf"), float("nan")
+    o, _, _ = sm.head_norm_rope(z, None, None, pos[:2], q_gamma=g)
+    assert not o[0, 0].any() and not o[1, 1].any() and not o[0, 1].isfinite().all() and o[1, 0].isnan().all()
+
+
+# ------------------------------------------------------------------------------------------------ attention
+
+def attn_case(lens, hq, hkv, d, page, dtype, seed=0, head_major=False, spare_cols=1, q_scale=1.0, scale=None, bad=(), poison=True, values=None):
+    g = torch.Generator().manual_seed(seed)
+    R = len(lens)
+    cols = max(1, max(-(-max(n, 0) // page) for n in lens) + spare_cols)
+    held = [min(cols, -(-max(n, 0) // page)) for n in lens]
+    n_pages = sum(held) + 3
+    ids = torch.randperm(n_pages, generator=g).tolist()
+    table = np.full((R, cols + 1), 10 ** 9)                        # (entries behind a request's pages are no page at all)
+    kp, vp = torch.randn(2, n_pages, page, hkv, d, generator=g)
+    if poison:                                                     # places behind the last token, and pages of nobody
+        kp[ids[-3]:ids[-3] + 1], vp[ids[-3]:ids[-3] + 1] = float("nan"), float("inf")
+    at = 0
+    for r in range(R):
+        table[r, :held[r]] = ids[at:at + held[r]]
+        at += held[r]
+        n = min(max(lens[r], 0), cols * page)
+        if poison and n % page:
+            kp[table[r, held[r] - 1], n % page:], vp[table[r, held[r] - 1], n % page:] = float("nan"), float("-inf")
+    for r, c, e in bad:
+        table[r, c] = e
+    kp, vp = kp.to(dtype), vp.to(dtype)
+    q = (torch.randn(R, hq + 1, d, generator=g) * q_scale).to(dtype)
+    s = d ** -0.5 if scale is None else scale
+    o, lse, av, aw = P.paged_attention(to_np(q)[:, :hq], to_np(kp), to_np(vp), table[:, :cols], lens, s, want_bound=True)
+    if head_major:
+        kd, vd = (t.transpose(1, 2).contiguous().cuda().transpose(1, 2) for t in (kp, vp))
+    else:
+        kd, vd = kp.cuda(), vp.cuda()
+    att = sm.PagedAttention(R, hq, hkv, d, page, cols, n_pages, dtype, scale=s)
+    att.ws.fill_(0xff)                                             # nothing in the workspace is taken for granted (NaN everywhere)
+    lse_d = torch.full((R, hq), 5.0, device="cuda")
+    out = torch.full((R, hq + 2, d), 9.0, dtype=dtype, device="cuda")
+    att(q.cuda()[:, :hq], kd, vd, ints(table)[:, :cols], ints(lens), out=out[:, 1:hq + 1], lse=lse_d)
+    torch.cuda.synchronize()
+    assert (out[:, 0] == 9).all() and (out[:, hq + 1] == 9).all()
+    n = max(max(lens), 1)
+    score = (d + 4) * 2.0 ** -24 * aw + (np.abs(np.where(np.isfinite(lse), lse, 0))[..., None] + 4) * 2.0 ** -23
+    weight = (2.0 ** -16 if dtype == BF16 else 2.0 ** -22) + (n / 16 + 64) * 2.0 ** -24
+    check(out[:, 1:hq + 1], o, HALF[dtype] * np.abs(o) + (2 * score + weight) * av, "o")
+    fin = np.isfinite(lse)
+    assert (to_np(lse_d)[~fin] == -np.inf).all() and (to_np(out[:, 1:hq + 1])[~fin] == 0).all()
+    check(lse_d[torch.from_numpy(fin).cuda()], lse[fin], (2 * score[..., 0] + weight + 2.0 ** -22 * (1 + np.abs(np.where(fin, lse, 0))))[fin], "lse")
+
+
+LENS = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hq,hkv,d", [(1, 1, 64), (4, 2, 128), (3, 1, 256), (16, 1, 64), (17, 1, 128), (10, 2, 96), (4, 4, 32), (8, 8, 8), (33, 1, 72), (5, 5, 248)])
+def test_paged_attention_heads(hq, hkv, d, dtype):
+    attn_case(LENS, hq, hkv, d, 16, dtype, seed=hq + d)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page", [1, 2, 3, 5, 8, 16, 24, 32, 48, 64, 100, 256])
+def test_paged_attention_pages(page, dtype):
+    attn_case(LENS + [4 * page, 4 * page + 1, 300], 4, 2, 64, page, dtype, seed=page, head_major=page % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lens,hq,hkv,d,page", [([5000], 8, 2, 128, 16), ([4097], 2, 2, 256, 64), ([1, 3000, 0, 7, 2047], 4, 1, 64, 8),
+                                                ([20000, 3], 2, 1, 64, 32), ([700] * 40, 4, 2, 64, 16), (list(range(300)), 2, 1, 32, 16)])
+def test_paged_attention_long_and_many(lens, hq, hkv, d, page, dtype):
+    attn_case(lens, hq, hkv, d, page, dtype, seed=len(lens))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_paged_attention_pages_that_are_not_there(dtype):
+    """Entries outside the pool stand for no page: their keys are left out; a request without any page gets zero and -inf."""
+    attn_case([100, 50, 16, 2000], 4, 2, 64, 16, dtype, bad=[(0, 0, -1), (0, 3, 10 ** 9), (1, 1, -2 ** 31), (2, 0, 2 ** 31 - 1), (3, 70, -5), (3, 0, 10 ** 6)])
+    attn_case([40, 64], 4, 2, 64, 8, dtype, bad=[(0, c, -1) for c in range(5)] + [(1, c, 10 ** 7) for c in range(8)])
+
+
+def test_paged_attention_lengths_outside_the_table():
+    for dtype in (BF16, F32):
+        attn_case([-3, 70, 2 ** 31 - 1, -2 ** 31][:2], 2, 1, 64, 16, dtype)
+    # lengths past the row end at the row's end
+    kp, vp = torch.randn(2, 8, 16, 1, 64, device="cuda")
+    q, t = torch.randn(3, 2, 64, device="cuda"), ints([[0, 1], [2, 3], [4, 5]])
+    att = sm.PagedAttention(3, 2, 1, 64, 16, 2, 8, F32)
+    assert torch.equal(att(q, kp, vp, t, ints([32, 33, 2 ** 31 - 1])), att(q, kp, vp, t, ints([32, 32, 32])))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_paged_attention_scales(dtype):
+    attn_case([300, 40], 4, 2, 64, 16, dtype, scale=0.0)
+    attn_case([300, 40], 4, 2, 64, 16, dtype, scale=-0.2)
+    attn_case([300, 700], 4, 2, 64, 16, dtype, q_scale=12.0)                # one key takes nearly all of the weight
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_paged_attention_infinite_and_nan_keys_stay_in_their_request(dtype):
+    g = torch.Generator().manual_seed(5)
+    kp, vp = torch.randn(2, 60, 16, 1, 64, generator=g).to(dtype).cuda()
+    q = torch.randn(3, 2, 64, generator=g).to(dtype).cuda()
+    table = ints(np.arange(60).reshape(3, 20).tolist())
+    att = sm.PagedAttention(3, 2, 1, 64, 16, 20, 60, dtype)
+    lens = ints([300, 300, 300])
+    want = att(q, kp, vp, table, lens).clone()
+    kp[21, 3] = float("nan")
+    vp[45, 3] = float("inf")
+    got = att(q, kp, vp, table, lens)
+    assert torch.equal(got[0], want[0]) and got[1].isnan().all() and (got[2] == float("inf")).all()
+
+
+def test_paged_attention_offsets_past_32_bits():
+    """A pool of more than 2^31 elements, only its last pages used."""
+    n_pages, page, hkv, d = 70000, 16, 8, 256
+    pool = torch.empty(n_pages, page, hkv, d, dtype=BF16, device="cuda")
+    assert pool.numel() > 2 ** 31
+    small = torch.randn(4, page, hkv, d, device="cuda").to(BF16)
+    pool[-4:] = small
+    q = torch.randn(2, 8, d, device="cuda").to(BF16)
+    lens = ints([20, 32])
+    big = sm.PagedAttention(2, 8, hkv, d, page, 2, n_pages, BF16)(q, pool, pool, ints([[69999, 69997], [69996, 69998]]), lens)
+    want = sm.PagedAttention(2, 8, hkv, d, page, 2, 4, BF16)(q, small, small, ints([[3, 1], [0, 2]]), lens)
+    assert torch.equal(big, want)
+    # and the store into it
+    x = torch.randn(3, hkv, d, device="cuda").to(BF16)
+    slots = [69999 * 16 + 5, 69996 * 16, 0]
+    sm.head_norm_rope(None, x, x, ints([0, 0, 0]), norm="none", rot=0, slots=ints(slots), k_out=pool, v_out=pool)
+    assert torch.equal(pool.view(-1, hkv, d)[slots], x)
+
+
+def test_paged_attention_is_deterministic_and_free_of_its_neighbours():
+    """The same call gives the same bits; what other requests are in the batch, in the same number of tokens, changes rounding only."""
+    g = torch.Generator().manual_seed(6)
+    kp, vp = torch.randn(2, 400, 16, 2, 128, generator=g).to(BF16).cuda()
+    q = torch.randn(4, 8, 128, generator=g).to(BF16).cuda()
+    table = torch.randperm(400, generator=g).to(I32).cuda().reshape(4, 100)
+    att = sm.PagedAttention(4, 8, 2, 128, 16, 100, 400, BF16)
+    lens = ints([1600, 900, 3, 0])
+    a = att(q, kp, vp, table, lens).clone()
+    for _ in range(5):
+        assert torch.equal(att(q, kp, vp, table, lens), a)
+
+
+# ------------------------------------------------------------------------------------------------ together
+
+def serve(E, hq, hkv, d, page, dtype, prompts, steps, graph=False):
+    """Prompts of ragged lengths, then decode iterations: pages, projection, norm + rotation + store, attention, output Linear; the
+    attention's result compared with a full causal softmax over the whole sequence in float64."""
+    g = torch.Generator().manual_seed(E + hq)
+    R = len(prompts)
+    w = {n: (torch.randn(o, i, generator=g) * i ** -0.5).to(dtype).cuda() for n, o, i in (("qkv", (hq + 2 * hkv) * d, E), ("out", E, hq * d))}
+    qg, kg = ((1 + 0.1 * torch.randn(d, generator=g)).to(dtype).cuda() for _ in range(2))
+    total = [p + steps for p in prompts]
+    cols = max(-(-n // page) for n in total) + 1
+    n_pages = sum(-(-n // page) for n in total) + 2
+    free = torch.randperm(n_pages, generator=g).to(I32).cuda()
+    kp, vp = (torch.full((n_pages, page, hkv, d), float("nan"), dtype=dtype, device="cuda") for _ in range(2))
+    table = torch.full((R, cols), -1, dtype=I32, device="cuda")
+    x_all = torch.randn(R, max(total), E, generator=g).to(dtype).cuda()
+    att = sm.PagedAttention(R, hq, hkv, d, page, cols, n_pages, dtype)
+
+    def project(x):
+        return sm.linear(x, w["qkv"]).view(-1, hq + 2 * hkv, d)
+
+    def rows(x, pt):
+        y = project(x)
+        return sm.head_norm_rope(y[:, :hq], y[:, hq:hq + hkv], y[:, hq + hkv:], pt.positions, q_gamma=qg, k_gamma=kg, slots=pt.slots, k_out=kp, v_out=vp)[0]
+
+    cached, taken = torch.zeros(R, dtype=I32, device="cuda"), 0
+    T = sum(prompts) + 3                                              # (padding rows)
+    x = torch.zeros(T, E, dtype=dtype, device="cuda")
+    x[:T - 3] = torch.cat([x_all[r, :p] for r, p in enumerate(prompts)])
+    pt = sm.page_table(cached, ints(prompts), free, ints([n_pages]), table, page, n_pages, T)
+    rows(x, pt)
+    cached, taken = pt.lens, pt.need.item()
+    qkv64 = to_np(torch.cat([project(x_all[r, :n].contiguous()) for r, n in enumerate(total)]))
+    at = np.cumsum([0] + total)
+    fresh = ints([1] * R)
+
+    def step(x, cached, free, n_free):
+        pt = sm.page_table(cached, fresh, free, n_free, table, page, n_pages, R)
+        q = rows(x, pt)
+        o = att(q, kp, vp, table, pt.lens)
+        return pt, o, sm.linear(o.view(R, hq * d), w["out"])
+
+    if graph:                                                         # static inputs, one captured iteration, replayed
+        sx, sc, sf, sn = torch.zeros(R, E, dtype=dtype, device="cuda"), cached.clone(), torch.zeros_like(free), ints([0])
+        torch.cuda.synchronize()
+        cg = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(cg):
+            spt, so, sy = step(sx, sc, sf, sn)
+    for i in range(steps):
+        xi = torch.stack([x_all[r, p + i] for r, p in enumerate(prompts)])
+        if graph:
+            sx.copy_(xi)
+            sc.copy_(cached)
+            sf[:n_pages - taken].copy_(free[taken:])
+            sn.fill_(n_pages - taken)
+            cg.replay()
+            torch.cuda.synchronize()
+            pt, o, y = spt, so.clone(), sy.clone()
+            before = kp.clone(), vp.clone(), table.clone()
+            pe, oe, ye = step(xi, cached, free[taken:].contiguous(), ints([n_pages - taken]))       # the same, eager
+            assert torch.equal(o, oe) and torch.equal(y, ye) and all(torch.equal(a, b) for a, b in zip(pt, pe))
+            assert all(torch.equal(a.nan_to_num(), b.nan_to_num()) for a, b in zip(before, (kp, vp, table)))
+        else:
+            pt, o, y = step(xi, cached, free[taken:].contiguous(), ints([n_pages - taken]))
+        assert pt.lens.tolist() == [p + i + 1 for p in prompts] and y.isfinite().all()
+        taken += pt.need.item()
+        cached = pt.lens.clone()
+        for r, p in enumerate(prompts):
+            n = p + i + 1
+            z = qkv64[at[r]:at[r] + n]
+            k = P.rope(P.head_norm(z[:, hq:hq + hkv], "rms", to_np(kg), None, 1e-5), np.arange(n), d, 10000.0)
+            q = P.rope(P.head_norm(z[-1:, :hq], "rms", to_np(qg), None, 1e-5), [n - 1], d, 10000.0)[0]
+            k, v = (np.repeat(t, hq // hkv, 1).transpose(1, 0, 2)[None] for t in (k, z[:, hq + hkv:]))
+            want, prob = O.attention(q[None, :, None], k, v, d ** -0.5)
+            want = want[0, :, 0]
+            # keys and queries were rounded once more on the way to the pages: logits off by 2 * half a step of sum |q k|
+            aw = (np.abs(q[:, None] * k[0]).sum(-1).max(-1) * d ** -0.5)[:, None]
+            av = (np.abs(v[0]) * prob[0, :, 0][..., None]).sum(1)
+            tol = HALF[dtype] * np.abs(want) + (2 * 2.2 * HALF[dtype] * aw + 1e-4 * (dtype == BF16) + 1e-5) * av
+            check(o[r], want, tol, "step %d, request %d" % (i, r))
+
+
+@pytest.mark.parametrize("graph", [False, True])
+@pytest.mark.parametrize("E,hq,hkv,d,page,dtype", [(256, 4, 2, 64, 16, BF16), (128, 6, 1, 128, 8, BF16), (64, 4, 4, 32, 4, F32)])
+def test_serving_iterations(E, hq, hkv, d, page, dtype, graph):
+    serve(E, hq, hkv, d, page, dtype, prompts=[37, 1, 130, 16], steps=5, graph=graph)
+
+
+def test_two_objects_on_two_streams():
+    """Two attentions with workspaces of their own at the same time, each on its stream."""
+    g = torch.Generator().manual_seed(9)
+    kp, vp = torch.randn(2, 512, 16, 2, 128, generator=g).to(BF16).cuda()
+    q = torch.randn(2, 2, 8, 128, generator=g).to(BF16).cuda()
+    table = torch.randperm(512, generator=g).to(I32).cuda().reshape(2, 256)
+    lens = ints([4096, 4000])
+    atts = [sm.PagedAttention(2, 8, 2, 128, 16, 256, 512, BF16) for _ in range(2)]
+    want = [atts[0](q[i].contiguous(), kp, vp, table, lens).clone() for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty_like(want[0]) for _ in range(2)]
+    for _ in range(10):
+        for i in range(2):
+            atts[i](q[i], kp, vp, table, lens, out=outs[i], stream=streams[i])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_binding_refuses_wrong_tensors():
+    x = torch.randn(4, 2, 64, device="cuda")
+    pos = torch.zeros(4, dtype=I32, device="cuda")
+    with pytest.raises(TypeError):
+        sm.head_norm_rope(x, None, None, pos.long(), norm="none")
+    with pytest.raises(ValueError):
+        sm.head_norm_rope(x, None, None, pos[:3], norm="none")
+    with pytest.raises(ValueError):
+        sm.head_norm_rope(x.transpose(1, 2), None, None, pos, norm="none")
+    with pytest.raises(sm.SmError):
+        sm.head_norm_rope(x, None, None, pos)                                       # the norm needs its gain
+    att = sm.PagedAttention(4, 2, 1, 64, 16, 2, 8, F32)
+    kp = torch.randn(8, 16, 1, 64, device="cuda")
+    table = torch.zeros(4, 2, dtype=I32, device="cuda")
+    with pytest.raises(ValueError):
+        att(x, kp, kp[:7], table, pos)
+    with pytest.raises(TypeError):
+        att(x.to(BF16), kp, kp, table, pos)
+    with pytest.raises(ValueError):
+        att(x, kp, kp, table.t(), pos)
+    with pytest.raises(sm.SmError):
+        sm.PagedAttention(4, 3, 2, 64, 16, 2, 8, F32)

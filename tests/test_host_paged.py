@@ -1,0 +1,160 @@
+"""Host side of the paged-cache operators and the 4-bit Linear without a GPU: what is refused, and that it is refused before any
+pointer is looked at (the pointers here are made up)."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2404_13528_amd import binding as sm
+
+A = C.c_void_p(1 << 20)          # 16-byte aligned, never dereferenced: every call here is refused on the host
+ODD = C.c_void_p((1 << 20) + 2)
+
+
+def page_cfg(n_req=4, page=16, max_pages=8, n_pages=64, free_cap=32, max_tokens=10, table_pitch=8):
+    return sm.PageCfg(n_req, page, max_pages, n_pages, free_cap, max_tokens, table_pitch)
+
+
+def page_call(cfg, *ptrs):
+    return sm.lib().sm_page_table(C.byref(cfg) if cfg else None, *(ptrs or [A] * 10), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(n_req=0), -2), (dict(n_req=65537), -2), (dict(page=0), -2), (dict(max_pages=0), -2), (dict(n_pages=0), -2), (dict(free_cap=-1), -2),
+    (dict(max_tokens=-1), -2), (dict(table_pitch=7), -2), (dict(page=1 << 28), -2), (dict(max_tokens=(1 << 30) + 1), -2),
+    (dict(n_req=65536, max_pages=1 << 15, table_pitch=1 << 15), -2), (dict(n_pages=(1 << 26) + 1), -2)])
+def test_page_table_refuses_sizes(change, code):
+    assert page_call(page_cfg(**change)) == code and len(sm.lib().sm_last_error()) > 0
+
+
+def test_page_table_refuses_pointers():
+    assert page_call(None) == -1
+    for i in range(10):
+        assert page_call(page_cfg(), *[None if j == i else A for j in range(10)]) == -1
+        assert page_call(page_cfg(), *[ODD if j == i else A for j in range(10)]) == -1
+
+
+def rope_desc(**change):
+    d = sm.HeadNormRopeDesc()
+    v = dict(dtype=sm.SM_BF16, tokens=4, heads_q=4, heads_kv=2, d=64, norm=2, eps=1e-5, rot=64, rope_base=10000.0, page=16, n_pages=4,
+             q_gamma=A.value, k_gamma=A.value, q_beta=A.value, k_beta=A.value)
+    v.update(change)
+    for n, x in v.items():
+        if n.endswith("stride"):
+            for i, s in enumerate(x):
+                getattr(d, n)[i] = s
+        else:
+            setattr(d, n, x)
+    return d
+
+
+def rope_call(d, q=A, k=A, v=A, positions=A, slots=A, q_out=A, k_out=A, v_out=A):
+    return sm.lib().sm_head_norm_rope(C.byref(d) if d else None, q, k, v, positions, slots, q_out, k_out, v_out, None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype=2), -1), (dict(tokens=-1), -2), (dict(heads_q=0), -2), (dict(heads_kv=0), -2), (dict(d=60), -2), (dict(d=264), -2), (dict(d=0), -2),
+    (dict(rot=24), -2), (dict(rot=80), -2), (dict(rot=-16), -2), (dict(norm=3), -1), (dict(rope_base=0.5), -1), (dict(rope_base=float("nan")), -1),
+    (dict(page=0), -2), (dict(n_pages=0), -2), (dict(n_pages=(1 << 26) + 1), -2), (dict(q_gamma=None), -1), (dict(k_gamma=None), -1),
+    (dict(norm=1, q_beta=None), -1), (dict(norm=1, k_beta=None), -1), (dict(q_gamma=A.value + 8), -1), (dict(q_stride=(4, 64)), -2),
+    (dict(q_out_stride=(64, 12)), -2), (dict(k_stride=(64, 4)), -2), (dict(k_out_stride=(4, 0, 0)), -2), (dict(v_out_stride=(0, 0, 4)), -2),
+    (dict(dtype=sm.SM_F32, d=66), -2), (dict(dtype=sm.SM_F32, rot=12), -2)])
+def test_head_norm_rope_refuses(change, code):
+    assert rope_call(rope_desc(**change)) == code and len(sm.lib().sm_last_error()) > 0
+
+
+def test_head_norm_rope_refuses_pointers():
+    assert rope_call(None) == -1
+    assert rope_call(rope_desc(), q=None, k=None, v=None) == -1
+    for n in ("positions", "q_out", "k_out", "v_out"):
+        assert rope_call(rope_desc(), **{n: None}) == -1
+    for n in ("q", "k", "v", "positions", "slots", "q_out", "k_out", "v_out"):
+        assert rope_call(rope_desc(), **{n: ODD}) == -1
+    assert rope_call(rope_desc(tokens=0), positions=None) == 0          # nothing to do
+
+
+def attn_desc(**change):
+    d = sm.PagedAttentionDesc()
+    v = dict(dtype=sm.SM_BF16, n_req=4, heads_q=8, heads_kv=2, d=128, page=16, max_pages=8, n_pages=64, scale=0.1, table_pitch=8)
+    v.update(change)
+    for n, x in v.items():
+        if n.endswith("stride"):
+            for i, s in enumerate(x):
+                getattr(d, n)[i] = s
+        else:
+            setattr(d, n, x)
+    return d
+
+
+def attn_call(d, ptrs=None, ws_bytes=1 << 40):
+    p = [A] * 8 if ptrs is None else ptrs
+    return sm.lib().sm_paged_attention(C.byref(d) if d else None, *p, C.c_size_t(ws_bytes), None)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype=5), -1), (dict(n_req=-1), -2), (dict(n_req=65536), -2), (dict(heads_q=0), -2), (dict(heads_kv=0), -2), (dict(heads_kv=3), -2),
+    (dict(d=4), -2), (dict(d=260), -2), (dict(d=264), -2), (dict(page=0), -2), (dict(max_pages=0), -2), (dict(n_pages=0), -2), (dict(table_pitch=7), -2),
+    (dict(page=1 << 28), -2), (dict(n_pages=(1 << 26) + 1), -2), (dict(scale=float("inf")), -1), (dict(q_stride=(4, 0)), -2), (dict(o_stride=(0, 4)), -2),
+    (dict(k_stride=(4, 0, 0)), -2), (dict(v_stride=(0, 0, 2)), -2)])
+def test_paged_attention_refuses(change, code):
+    assert attn_call(attn_desc(**change)) == code and len(sm.lib().sm_last_error()) > 0
+    assert sm.lib().sm_paged_attention_workspace_bytes(C.byref(attn_desc(**change))) == 0
+
+
+def test_paged_attention_refuses_pointers_and_small_workspaces():
+    assert attn_call(None) == -1
+    for i in (0, 1, 2, 3, 4, 5, 7):
+        assert attn_call(attn_desc(), [None if j == i else A for j in range(8)]) == -1
+    for i in range(8):
+        assert attn_call(attn_desc(), [ODD if j == i else A for j in range(8)]) == -1
+    need = sm.lib().sm_paged_attention_workspace_bytes(C.byref(attn_desc()))
+    assert 0 < need and attn_call(attn_desc(), ws_bytes=need - 1) == -4
+    assert attn_call(attn_desc(n_req=0), [None] * 8, 0) == 0
+
+
+def test_paged_attention_workspace_is_bounded():
+    """Partial results: some per workgroup, not some per page of the longest request."""
+    for d in (attn_desc(n_req=256, max_pages=8192, table_pitch=8192, heads_q=64, heads_kv=8), attn_desc(n_req=1, max_pages=65536, table_pitch=65536, page=64)):
+        assert sm.lib().sm_paged_attention_workspace_bytes(C.byref(d)) < 256 << 20
+
+
+@pytest.mark.parametrize("N,K,group,taken", [(1, 32, 32, True), (7, 192, 64, True), (4096, 4096, 128, True), (0, 64, 32, False), (8, 96, 64, False), (8, 64, 16, False),
+                                             (8, 64, 256, False), (8, 0, 32, False), ((1 << 24) + 1, 32, 32, False)])
+def test_w4_sizes(N, K, group, taken):
+    n = sm.lib().sm_linear_w4_packed_bytes(N, K, group)
+    assert (n > 0) == taken
+    if taken:                      # weights, scales and zero points, the rows rounded up to whole tiles
+        assert n >= N * K // 2 + 3 * N * (K // group)
+    else:
+        d = sm.LinearW4Desc(1, N, K, group, 0)
+        assert sm.lib().sm_linear_w4(C.byref(d), A, A, A, A, A, None) < 0 and len(sm.lib().sm_last_error()) > 0
+        assert sm.lib().sm_linear_w4_pack(A, A, A, N, K, group, A, None) < 0
+
+
+def test_w4_refuses_pointers():
+    lib, d = sm.lib(), sm.LinearW4Desc(2, 64, 128, 128, 0)
+    assert lib.sm_linear_w4(None, A, A, A, A, A, None) == -1
+    for i in (0, 1, 4):
+        assert lib.sm_linear_w4(C.byref(d), *[None if j == i else A for j in range(5)], None) == -1
+    for i in range(5):
+        assert lib.sm_linear_w4(C.byref(d), *[ODD if j == i else A for j in range(5)], None) == -1
+    for i in (0, 1, 3):
+        p = [A, A, A, A]
+        p[i] = None
+        assert lib.sm_linear_w4_pack(p[0], p[1], p[2], 64, 128, 128, p[3], None) == -1
+    assert lib.sm_linear_w4(C.byref(sm.LinearW4Desc(2, 64, 128, 128, 2)), A, A, A, A, A, None) == -3
+    assert lib.sm_linear_w4(C.byref(sm.LinearW4Desc(-1, 64, 128, 128, 0)), A, A, A, A, A, None) == -2
+    assert lib.sm_linear_w4(C.byref(sm.LinearW4Desc(0, 64, 128, 128, 0)), None, None, None, None, None, None) == 0
+
+
+def test_binding_refuses_host_tensors():
+    i32 = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        sm.page_table(i32, i32, i32, i32[:1], i32.reshape(4, 1), 16, 4, 4)
+    x = torch.zeros(4, 2, 64)
+    with pytest.raises(ValueError):
+        sm.head_norm_rope(x, None, None, i32)
+    with pytest.raises(ValueError):
+        sm.head_norm_rope(None, None, None, i32)
+    with pytest.raises(ValueError):
+        sm.LinearW4(torch.zeros(8, 16, dtype=torch.uint8), torch.zeros(8, 1, dtype=torch.bfloat16), group=32)
