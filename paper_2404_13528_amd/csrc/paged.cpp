@@ -9,6 +9,14 @@ using namespace sm;
 namespace {
 constexpr int64_t CAP = (int64_t)1 << 30;
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+// the last place of a page pool in units of 16 bytes, -1 if it does not fit 32 bits or a stride is negative
+int64_t pool_units(const int64_t (&s)[3], int n_pages, int page, int vec) {
+  const int64_t top = (int64_t)1 << 32;
+  if (s[0] < 0 || s[1] < 0 || s[0] / vec >= top || s[1] / vec >= top) return -1;
+  const int64_t u = (int64_t)(n_pages - 1) * (s[0] / vec);          // (both factors below 2^30 resp. 2^32)
+  const int64_t v = (int64_t)(page - 1) * (s[1] / vec);
+  return u < top && v < top && u + v < top ? u + v : -1;
+}
 template <int N> bool multiples(const int64_t (&s)[N], int vec) {
   for (int64_t v : s) if (v % vec) return false;
   return true;
@@ -100,6 +108,9 @@ int check_paged_attention(const sm_paged_attention_desc* c, const char* who) {
   if (!std::isfinite(c->scale)) return fail(SM_ERR_INVALID_ARG, "%s: the scale must be finite", who);
   if (!multiples(c->q_stride, vec) || !multiples(c->o_stride, vec) || !multiples(c->k_stride, vec) || !multiples(c->v_stride, vec))
     return fail(SM_ERR_SHAPE, "%s: strides must keep 16-byte alignment", who);
+  const int64_t last[2] = {pool_units(c->k_stride, c->n_pages, c->page, vec), pool_units(c->v_stride, c->n_pages, c->page, vec)};
+  if (last[0] < 0 || last[1] < 0) return fail(SM_ERR_SHAPE, "%s: a pool has strides of at least zero and spans at most 64 GiB", who);
+  if (!paged_attention_fits(c->n_req, c->heads_q, c->heads_kv, (int64_t)c->page * c->max_pages)) return fail(SM_ERR_SHAPE, "%s: too many requests and heads for one launch", who);
   return SM_OK;
 }
 }  // namespace

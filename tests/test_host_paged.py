@@ -95,7 +95,9 @@ def attn_call(d, ptrs=None, ws_bytes=1 << 40):
     (dict(dtype=5), -1), (dict(n_req=-1), -2), (dict(n_req=65536), -2), (dict(heads_q=0), -2), (dict(heads_kv=0), -2), (dict(heads_kv=3), -2),
     (dict(d=4), -2), (dict(d=260), -2), (dict(d=264), -2), (dict(page=0), -2), (dict(max_pages=0), -2), (dict(n_pages=0), -2), (dict(table_pitch=7), -2),
     (dict(page=1 << 28), -2), (dict(n_pages=(1 << 26) + 1), -2), (dict(scale=float("inf")), -1), (dict(q_stride=(4, 0)), -2), (dict(o_stride=(0, 4)), -2),
-    (dict(k_stride=(4, 0, 0)), -2), (dict(v_stride=(0, 0, 2)), -2)])
+    (dict(k_stride=(4, 0, 0)), -2), (dict(v_stride=(0, 0, 2)), -2), (dict(k_stride=(-8, 0, 0)), -2), (dict(v_stride=(0, -128, 0)), -2),
+    (dict(k_stride=(1 << 35, 128, 128)), -2), (dict(v_stride=((1 << 35) // 63 + 8 - (1 << 35) // 63 % 8, 0, 0)), -2),
+    (dict(n_req=65535, heads_q=65535, heads_kv=65535), -2)])
 def test_paged_attention_refuses(change, code):
     assert attn_call(attn_desc(**change)) == code and len(sm.lib().sm_last_error()) > 0
     assert sm.lib().sm_paged_attention_workspace_bytes(C.byref(attn_desc(**change))) == 0
