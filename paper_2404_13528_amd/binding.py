@@ -8,6 +8,7 @@ torch is used for device memory and streams only.
 import collections
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsmartmem.so")
@@ -134,6 +135,10 @@ def lib():
                   "sm_cswin_attention_workspace_bytes", "sm_cswin_block_workspace_bytes", "sm_paged_attention_workspace_bytes",
                   "sm_linear_w4_packed_bytes"):
             getattr(L, f).restype = C.c_size_t
+        p, i = C.c_void_p, C.c_int                # calls that take their addresses as plain integers
+        for f, args in (("sm_page_table", [p] * 12), ("sm_head_norm_rope", [p] * 10), ("sm_paged_attention", [p] * 9 + [C.c_size_t, p]),
+                        ("sm_linear_w4_pack", [p] * 3 + [i] * 3 + [p] * 2), ("sm_linear_w4", [p] * 7)):
+            getattr(L, f).argtypes = args
         _lib = L
     return _lib
 
@@ -777,24 +782,72 @@ class DecodeStep:
 # a paged key / value cache and the Linears around it
 # --------------------------------------------------------------------------
 
-def _take(t, name, dtype, shape=None, device=None, rows=False):
-    """Checks a device tensor before its address goes to the library: dtype, shape (None: any extent), one device, and a
-    contiguous last axis (rows=True) or contiguous throughout."""
+# (A decode iteration makes these calls once per layer and they run for a few microseconds: what is right is found right by a few
+# comparisons, plain integers go to the library, and only a call that is refused pays for saying why.)
+
+def _refuse(t, name, dtype, shape, device, rows):
     import torch
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("%s must be a tensor on the GPU" % name)
-    if t.device.index != torch.cuda.current_device() or (device is not None and t.device != device):
-        raise ValueError("%s is on %s: all tensors of a call belong to the current device" % (name, t.device))
+    if t.device != device:
+        raise ValueError("%s is on %s: all tensors of a call belong to the current device, %s" % (name, t.device, device))
     if t.dtype != dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if shape is not None and (t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape))):
-        raise ValueError("%s must have the shape %s, not %s" % (name, tuple("any" if w is None else w for w in shape), tuple(t.shape)))
-    if rows:
-        if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError("the last axis of %s must be contiguous" % name)
-    elif not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
-    return t
+    if t.shape != shape:
+        raise ValueError("%s must have the shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+    raise ValueError("the last axis of %s must be contiguous" % name if rows else "%s must be contiguous" % name)
+
+
+def _flat(t, name, dtype, shape, device):
+    """The address of a contiguous device tensor of that type and shape."""
+    try:
+        if t.dtype == dtype and t.shape == shape and t.device == device and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, name, dtype, shape, device, False)
+
+
+def _rows(t, name, dtype, shape, device):
+    """The address of a device tensor of that type and shape whose last axis is contiguous."""
+    try:
+        if t.dtype == dtype and t.shape == shape and t.device == device and (shape[-1] == 1 or t.stride(-1) == 1):
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(t, name, dtype, shape, device, True)
+
+
+_devices = {}
+
+
+def _device():
+    """The current device."""
+    import torch
+    try:
+        i = torch.cuda.current_device()
+    except (RuntimeError, AssertionError) as e:
+        raise ValueError("tensors on a GPU are needed: %s" % e)
+    d = _devices.get(i)
+    if d is None:
+        d = _devices[i] = torch.device("cuda", i)
+    return d
+
+
+def _raw_stream(device, stream):
+    import torch
+    if stream is not None:
+        return stream.cuda_stream
+    try:                                          # (the number alone: a tenth of the time of a Stream object)
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    except AttributeError:
+        return torch.cuda.current_stream(device).cuda_stream
+
+
+def _dims(t, name, n):
+    if getattr(t, "ndim", None) != n:
+        raise ValueError("%s must be a tensor of %d axes" % (name, n))
+    return t.shape
 
 
 class PageCfg(C.Structure):
@@ -807,23 +860,20 @@ PageTable = collections.namedtuple("PageTable", "starts lens positions slots nee
 def page_table(cached, fresh, free_pages, n_free, table, page, n_pages, max_tokens, out=None, stream=None):
     """sm_page_table: pages and slots of the new tokens of an iteration, from lengths on the device.  cached, fresh [R], free_pages,
     n_free [1] and table [R, max_pages] (updated in place) are int32 device tensors.  Returns PageTable(starts [R + 1], lens [R],
-    positions [max_tokens], slots [max_tokens], need [1]), or fills the one given as `out`."""
+    positions [max_tokens], slots [max_tokens], need [1]) (parts of one new tensor), or fills the one given as `out`."""
     import torch
-    i32 = torch.int32
-    R = _take(cached, "cached", i32, (None,)).shape[0]
-    _take(fresh, "fresh", i32, (R,))
-    _take(free_pages, "free_pages", i32, (None,))
-    _take(n_free, "n_free", i32, (1,))
-    _take(table, "table", i32, (R, None), rows=True)
-    max_tokens = int(max_tokens)
-    shapes = {"starts": R + 1, "lens": R, "positions": max_tokens, "slots": max_tokens, "need": 1}
+    i32, dev = torch.int32, _device()
+    R, cols = _dims(table, "table", 2)
+    free_cap, = _dims(free_pages, "free_pages", 1)
+    n = max(0, int(max_tokens))
+    cfg = PageCfg(R, int(page), cols, int(n_pages), free_cap, int(max_tokens), table.stride(0) if R > 1 else cols)
+    ins = (_flat(cached, "cached", i32, (R,), dev), _flat(fresh, "fresh", i32, (R,), dev), _flat(free_pages, "free_pages", i32, (free_cap,), dev),
+           _flat(n_free, "n_free", i32, (1,), dev), _rows(table, "table", i32, (R, cols), dev))
+    sizes = (R + 1, R, n, n, 1)
     if out is None:
-        out = PageTable(*[torch.empty(max(0, n), dtype=i32, device=cached.device) for n in shapes.values()])
-    for name, n in shapes.items():
-        _take(getattr(out, name), name, i32, (n,))
-    cfg = PageCfg(R, int(page), table.shape[1], int(n_pages), free_pages.shape[0], max_tokens, table.stride(0) if R > 1 else table.shape[1])
-    check(lib().sm_page_table(C.byref(cfg), _ptr(cached), _ptr(fresh), _ptr(free_pages), _ptr(n_free), _ptr(table), _ptr(out.starts),
-                              _ptr(out.lens), _ptr(out.positions), _ptr(out.slots), _ptr(out.need), _stream(stream)), "sm_page_table")
+        out = PageTable(*torch.empty(sum(sizes), dtype=i32, device=dev).split(sizes))
+    ptrs = [_flat(t, name, i32, (k,), dev) for t, name, k in zip(out, PageTable._fields, sizes)]
+    check(lib().sm_page_table(C.byref(cfg), *ins, *ptrs, _raw_stream(dev, stream)), "sm_page_table")
     return out
 
 
@@ -834,6 +884,7 @@ class HeadNormRopeDesc(C.Structure):
                [(n, C.c_int64 * 3) for n in ("k_out_stride", "v_out_stride")]
 
 
+_HEAD_NORM_ROPE = struct.Struct("@6if4Pif2i14q")          # HeadNormRopeDesc in one step
 HEAD_NORM = {"none": 0, "layer": 1, "rms": 2}
 
 
@@ -844,48 +895,39 @@ def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gam
     of the pools k_out / v_out [n_pages, page, heads_kv, d] (strided views, so a head-major pool is passed permuted); without slots
     k_out / v_out are [T, heads_kv, d] (new tensors by default), as q_out always is.  Returns (q_out, k_out, v_out)."""
     import torch
-    first = next((t for t in (q, k, v) if t is not None), None)
+    first = q if q is not None else k if k is not None else v
     if first is None:
         raise ValueError("q, k and v are all None")
-    if first.dim() != 3:
-        raise ValueError("q, k and v have three axes: token, head, feature")
-    dt, dev, (T, _, d) = first.dtype, first.device, first.shape
-    desc = HeadNormRopeDesc()
-    desc.dtype, desc.tokens, desc.d, desc.norm, desc.eps = _dt(first), T, d, HEAD_NORM[norm], eps
-    desc.rot, desc.rope_base = d if rot is None else int(rot), rope_base
-    _take(positions, "positions", torch.int32, (T,), dev)
+    T, heads, d = _dims(first, "q" if q is not None else "k" if k is not None else "v", 3)
+    dt, dev, i32 = first.dtype, _device(), torch.int32
+    hq, hkv = (heads if q is not None else 0), (0 if k is None and v is None else _dims(k if k is not None else v, "k" if k is not None else "v", 3)[1])
+    pos = _flat(positions, "positions", i32, (T,), dev)
+    at, n_pages, page, kv_shape = None, 0, 0, (T, hkv, d)
     if slots is not None:
-        _take(slots, "slots", torch.int32, (T,), dev)
-        pool = k_out if k is not None else v_out
-        if pool is None or pool.dim() != 4:
-            raise ValueError("slots need the page pools k_out / v_out [n_pages, page, heads_kv, d]")
-        desc.n_pages, desc.page = pool.shape[:2]
-    kv = next((t for t in (k, v) if t is not None), None)
-    desc.heads_kv = 0 if kv is None else kv.shape[1]
-    desc.heads_q = 0 if q is None else q.shape[1]
-    outs = []
-    for n, x, y, heads in (("q", q, q_out, desc.heads_q), ("k", k, k_out, desc.heads_kv), ("v", v, v_out, desc.heads_kv)):
+        at = _flat(slots, "slots", i32, (T,), dev)
+        if k is not None or v is not None:
+            n_pages, page = _dims(k_out if k is not None else v_out, "the page pool of k / v", 4)[:2]
+            kv_shape = (n_pages, page, hkv, d)
+    xs, ys, in_st, out_st, outs = [], [], [], [], []
+    for name, x, y, shape in (("q", q, q_out, (T, hq, d)), ("k", k, k_out, kv_shape), ("v", v, v_out, kv_shape)):
+        plain = name == "q" or slots is None
         if x is None:
-            outs.append(None)
+            xs.append(None), ys.append(None), outs.append(None)
+            in_st += (0, 0)
+            out_st += (0, 0) if name == "q" else (0, 0, 0)
             continue
-        _take(x, n, dt, (T, heads, d), dev, rows=True)
-        paged = slots is not None and n != "q"
-        if y is None and not paged:
-            y = torch.empty((T, heads, d), dtype=dt, device=dev)
-        _take(y, n + "_out", dt, (desc.n_pages, desc.page, heads, d) if paged else (T, heads, d), dev, rows=True)
+        xs.append(_rows(x, name, dt, (T, shape[-2], d), dev))
+        if y is None and plain:
+            y = torch.empty(shape, dtype=dt, device=dev)
+        ys.append(_rows(y, name + "_out", dt, shape, dev))
         outs.append(y)
-        for i in range(2):
-            getattr(desc, n + "_stride")[i] = x.stride(i)
-        st = [s for s in y.stride()[:-1]]
-        for i, s in enumerate(st if n == "q" or paged else [0] + st):
-            getattr(desc, n + "_out_stride")[i] = s
-        if n != "v":
-            for part, g in (("gamma", q_gamma if n == "q" else k_gamma), ("beta", q_beta if n == "q" else k_beta)):
-                if g is not None:
-                    _take(g, "%s_%s" % (n, part), dt, (d,), dev)
-                setattr(desc, "%s_%s" % (n, part), _ptr(g).value)
-    check(lib().sm_head_norm_rope(C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(positions), _ptr(slots), _ptr(outs[0]), _ptr(outs[1]),
-                                  _ptr(outs[2]), _stream(stream)), "sm_head_norm_rope")
+        in_st += x.stride()[:2]
+        out_st += y.stride()[:-1] if name == "q" or not plain else (0,) + y.stride()[:2]
+    gains = [0 if g is None else _flat(g, name, dt, (d,), dev)
+             for name, g in (("q_gamma", q_gamma), ("q_beta", q_beta), ("k_gamma", k_gamma), ("k_beta", k_beta))]
+    desc = _HEAD_NORM_ROPE.pack(_dt(first), T, hq, hkv, d, HEAD_NORM[norm], eps, *gains, d if rot is None else int(rot), rope_base, page, n_pages,
+                                *in_st, *out_st)
+    check(lib().sm_head_norm_rope(desc, *xs, pos, at, *ys, _raw_stream(dev, stream)), "sm_head_norm_rope")
     return tuple(outs)
 
 
@@ -901,6 +943,8 @@ class PagedAttention:
 
     def __init__(self, n_req, heads_q, heads_kv, d, page, max_pages, n_pages, dtype, scale=None):
         import torch
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("unsupported dtype %s" % dtype)
         c = PagedAttentionDesc()
         c.dtype = SM_F32 if dtype == torch.float32 else SM_BF16
         c.n_req, c.heads_q, c.heads_kv, c.d, c.page, c.max_pages, c.n_pages = n_req, heads_q, heads_kv, d, page, max_pages, n_pages
@@ -911,28 +955,20 @@ class PagedAttention:
         if n == 0:
             raise SmError("sm_paged_attention_workspace_bytes: " + lib().sm_last_error().decode())
         self.ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        self.q_shape, self.pool_shape, self.table_shape = (n_req, heads_q, d), (n_pages, page, heads_kv, d), (n_req, max_pages)
 
     def __call__(self, q, k_pages, v_pages, table, lens, out=None, lse=None, stream=None):
         import torch
-        c, dt, dev = self.desc, self.dtype, self.ws.device
-        _take(q, "q", dt, (c.n_req, c.heads_q, c.d), dev, rows=True)
-        for n, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-            _take(t, n, dt, (c.n_pages, c.page, c.heads_kv, c.d), dev, rows=True)
-        _take(table, "table", torch.int32, (c.n_req, c.max_pages), dev, rows=True)
-        _take(lens, "lens", torch.int32, (c.n_req,), dev)
+        c, dt, dev, i32 = self.desc, self.dtype, _device(), torch.int32
         if out is None:
-            out = torch.empty((c.n_req, c.heads_q, c.d), dtype=dt, device=dev)
-        _take(out, "out", dt, (c.n_req, c.heads_q, c.d), dev, rows=True)
-        if lse is not None:
-            _take(lse, "lse", torch.float32, (c.n_req, c.heads_q), dev)
-        d = PagedAttentionDesc.from_buffer_copy(c)
-        d.table_pitch = table.stride(0) if c.n_req > 1 else c.max_pages
-        for i in range(2):
-            d.q_stride[i], d.o_stride[i] = q.stride(i), out.stride(i)
-        for i in range(3):
-            d.k_stride[i], d.v_stride[i] = k_pages.stride(i), v_pages.stride(i)
-        check(lib().sm_paged_attention(C.byref(d), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(table), _ptr(lens), _ptr(out), _ptr(lse),
-                                       _ptr(self.ws), C.c_size_t(self.ws.numel()), _stream(stream)), "sm_paged_attention")
+            out = torch.empty(self.q_shape, dtype=dt, device=dev)
+        args = (_rows(q, "q", dt, self.q_shape, dev), _rows(k_pages, "k_pages", dt, self.pool_shape, dev), _rows(v_pages, "v_pages", dt, self.pool_shape, dev),
+                _rows(table, "table", i32, self.table_shape, dev), _flat(lens, "lens", i32, self.q_shape[:1], dev), _rows(out, "out", dt, self.q_shape, dev),
+                None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(self.ws, "the workspace", torch.uint8, self.ws.shape, dev))
+        c.table_pitch = table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1]
+        c.q_stride[:], c.o_stride[:] = q.stride()[:2], out.stride()[:2]
+        c.k_stride[:], c.v_stride[:] = k_pages.stride()[:3], v_pages.stride()[:3]
+        check(lib().sm_paged_attention(C.byref(c), *args, self.ws.numel(), _raw_stream(dev, stream)), "sm_paged_attention")
         return out
 
 
@@ -947,30 +983,31 @@ class LinearW4:
 
     def __init__(self, w, scales, zeros=None, group=128, bias=None, stream=None):
         import torch
-        N, K = _take(w, "w", torch.uint8, (None, None)).shape[0], 2 * w.shape[1]
-        n = lib().sm_linear_w4_packed_bytes(N, K, int(group))
+        u8, dev, group = torch.uint8, _device(), int(group)
+        N, half = _dims(w, "w", 2)
+        wp = _flat(w, "w", u8, (N, half), dev)
+        n = lib().sm_linear_w4_packed_bytes(N, 2 * half, group)
         if n == 0:
             raise SmError("sm_linear_w4_packed_bytes: " + lib().sm_last_error().decode())
-        _take(scales, "scales", torch.bfloat16, (N, K // group), w.device)
-        if zeros is not None:
-            _take(zeros, "zeros", torch.uint8, (N, K // group), w.device)
+        shape = (N, 2 * half // group)
+        sp, zp = _flat(scales, "scales", torch.bfloat16, shape, dev), None if zeros is None else _flat(zeros, "zeros", u8, shape, dev)
         if bias is not None:
-            _take(bias, "bias", torch.bfloat16, (N,), w.device)
-        self.N, self.K, self.group, self.bias = N, K, int(group), bias
-        self.packed = torch.empty(n, dtype=torch.uint8, device=w.device)
-        check(lib().sm_linear_w4_pack(_ptr(w), _ptr(scales), _ptr(zeros), N, K, self.group, _ptr(self.packed), _stream(stream)), "sm_linear_w4_pack")
+            _flat(bias, "bias", torch.bfloat16, (N,), dev)
+        self.N, self.K, self.group, self.bias = N, 2 * half, group, bias
+        self.packed = torch.empty(n, dtype=u8, device=dev)
+        check(lib().sm_linear_w4_pack(wp, sp, zp, N, self.K, group, self.packed.data_ptr(), _raw_stream(dev, stream)), "sm_linear_w4_pack")
 
     def __call__(self, x, residual=None, act="none", out=None, stream=None):
         import torch
-        bf16, dev = torch.bfloat16, self.packed.device
-        M = _take(x, "x", bf16, (None, self.K), dev).shape[0]
-        if residual is not None:
-            _take(residual, "residual", bf16, (M, self.N), dev)
+        bf16, dev = torch.bfloat16, _device()
+        M, _ = _dims(x, "x", 2)
+        xp, shape = _flat(x, "x", bf16, (M, self.K), dev), (M, self.N)
         if out is None:
-            out = torch.empty((M, self.N), dtype=bf16, device=dev)
-        _take(out, "out", bf16, (M, self.N), dev)
+            out = torch.empty(shape, dtype=bf16, device=dev)
         d = LinearW4Desc(M, self.N, self.K, self.group, ACT[act])
-        check(lib().sm_linear_w4(C.byref(d), _ptr(x), _ptr(self.packed), _ptr(self.bias), _ptr(residual), _ptr(out), _stream(stream)), "sm_linear_w4")
+        check(lib().sm_linear_w4(C.byref(d), xp, _flat(self.packed, "the packed weights", torch.uint8, self.packed.shape, dev),
+                                 None if self.bias is None else self.bias.data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev),
+                                 _flat(out, "out", bf16, shape, dev), _raw_stream(dev, stream)), "sm_linear_w4")
         return out
 
 
