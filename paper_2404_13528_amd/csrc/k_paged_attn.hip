@@ -5,8 +5,8 @@
 // length, such that about PA_ITEMS workgroups have one each, whatever the mix of short and long requests; every wave finds
 // its workgroup's chunk with one scan over the lengths.  Chunks of a request are joined by a second, small kernel.
 //
-//  * A wave takes tiles of 32 (bf16) or 16 (fp32) keys straight from memory into registers, the next tile requested before
-//    the present one is used; there is no LDS on the way and no barrier in the loop.
+//  * A wave takes tiles of 32 (bf16) or 16 (fp32) keys straight from memory into registers, the next keys and values requested
+//    as soon as the present ones are used up; there is no LDS on the way and no barrier in the loop.
 //  * S^T = K Q^T on the matrix pipe: K is the first operand as it lies in memory, the up to 16 query heads of a key head are
 //    the columns.  The result has four keys per lane, column = query: softmax statistics are sums over a lane's values and
 //    two steps between lanes.
@@ -96,39 +96,41 @@ template <typename T, int DP> struct PaTile {
   unsigned v[NV][VW];
 };
 struct PaWhere { unsigned k, v; bool on; };                 // place of this lane's key of a tile in units of 16 bytes, and whether it is there
+struct PaUnits { unsigned k_page, k_t, v_page, v_t; };      // strides of the pools in units of 16 bytes
 
-// the place of key `key` of request r; keys that are not there get the pool's first place
-__device__ __forceinline__ PaWhere pa_where(const PagedAttnArgs& a, const int* row, int key, int k1, unsigned ku_page, unsigned ku_t,
-                                              unsigned vu_page, unsigned vu_t) {
-  PaWhere w = {0, 0, false};
-  if (key < k1) {
-    const int pg = key / a.page, in = key - pg * a.page, id = row[pg];
-    if (id >= 0 && id < a.n_pages) {
-      w.k = (unsigned)id * ku_page + (unsigned)in * ku_t;
-      w.v = (unsigned)id * vu_page + (unsigned)in * vu_t;
-      w.on = true;
-    }
-  }
+// the place of a key whose page table entry is `id`; keys that are not there get the pool's first place
+__device__ __forceinline__ PaWhere pa_where(const PagedAttnArgs& a, const PaUnits& u, int id, int key, int k1) {
+  const unsigned in = (unsigned)key % (unsigned)a.page;
+  PaWhere w;
+  w.on = key < k1 && id >= 0 && id < a.n_pages;
+  w.k = w.on ? (unsigned)id * u.k_page + in * u.k_t : 0;
+  w.v = w.on ? (unsigned)id * u.v_page + in * u.v_t : 0;
   return w;
 }
 
 template <typename T, int DP, bool FULL>
-__device__ __forceinline__ void pa_load(PaTile<T, DP>& t, const PaWhere& w, const char* kb, const char* vb, const int d) {
+__device__ __forceinline__ void pa_load_k(PaTile<T, DP>& t, const unsigned where, const char* kb, const int d) {
   typedef PaTile<T, DP> Tile;
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   constexpr int SUB = Tile::TK / 16, STEPS = Tile::NK / SUB, E = 16 / (int)sizeof(T);
 #pragma unroll
   for (int j = 0; j < SUB; ++j) {
-    const char* p = kb + (uint64_t)__shfl(w.k, 16 * j + c, 64) * 16 + g * 16;
+    const char* p = kb + (uint64_t)__shfl(where, 16 * j + c, 64) * 16 + g * 16;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       if (FULL || (s * 4 + g) * E < d) t.k[j * STEPS + s] = *(const pa_u32x4*)(p + s * 64);
       else t.k[j * STEPS + s] = pa_u32x4{0, 0, 0, 0};
     }
   }
+}
+template <typename T, int DP, bool FULL>
+__device__ __forceinline__ void pa_load_v(PaTile<T, DP>& t, const unsigned where, const char* vb, const int d) {
+  typedef PaTile<T, DP> Tile;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  constexpr int E = 16 / (int)sizeof(T);
 #pragma unroll
   for (int i = 0; i < Tile::NV; ++i) {
-    const char* p = vb + (uint64_t)__shfl(w.v, 16 * (i / 4) + 4 * g + (i & 3), 64) * 16 + c * Tile::VW * 4;
+    const char* p = vb + (uint64_t)__shfl(where, 16 * (i / 4) + 4 * g + (i & 3), 64) * 16 + c * Tile::VW * 4;
     if constexpr (Tile::VW == 2) {
       pa_u32x2 x = {0, 0};
       if (FULL || c * Tile::EV < d) x = *(const pa_u32x2*)p;
@@ -152,27 +154,39 @@ __device__ __forceinline__ pa_f32x4 pa_mfma1(unsigned a, unsigned b, pa_f32x4 c)
   return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
 }
 
-// one tile: q [NK / SUB] the query operand, mask the keys that are there (bit = key)
-template <typename T, int DP>
-__device__ __forceinline__ void pa_tile(PaTile<T, DP>& t, const pa_u32x4* q, const unsigned mask, const float scale, float& m, float& l, pa_f32x4* o) {
+// features e .. of query lane % 16
+template <typename T>
+__device__ __forceinline__ pa_u32x4 pa_query(const PagedAttnArgs& a, int r, int h0, int rows, int e) {
+  const int c = threadIdx.x & 15;
+  if (c >= rows || e >= a.d) return pa_u32x4{0, 0, 0, 0};
+  return *(const pa_u32x4*)((const T*)a.q + (int64_t)r * a.q_r + (int64_t)(h0 + c) * a.q_h + e);
+}
+// logits of a tile, times log2 e: q(step) is the query operand; a lane gets keys 4 (lane / 16) + i (+ 16) of query lane % 16
+template <typename T, int DP, typename Q>
+__device__ __forceinline__ void pa_logits(const PaTile<T, DP>& t, const Q& q, const float scale, float* s) {
   typedef PaTile<T, DP> Tile;
-  constexpr int SUB = Tile::TK / 16, STEPS = Tile::NK / SUB, NV = Tile::NV;
-  const int g = (threadIdx.x & 63) >> 4;
-  float s[NV];
+  constexpr int SUB = Tile::TK / 16, STEPS = Tile::NK / SUB;
 #pragma unroll
   for (int j = 0; j < SUB; ++j) {
     pa_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
-      if constexpr (sizeof(T) == 2) acc = pa_mfma(t.k[j * STEPS + i], q[i], acc);
+      if constexpr (sizeof(T) == 2) acc = pa_mfma(t.k[j * STEPS + i], q(i), acc);
       else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc = pa_mfma1(t.k[i][e], q[i][e], acc);
+        for (int e = 0; e < 4; ++e) acc = pa_mfma1(t.k[i][e], q(i)[e], acc);
       }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[4 * j + i] = acc[i] * scale;
   }
+}
+// weights and values of a tile into the running maximum, sum and result; mask: the keys that are there (bit = key)
+template <typename T, int DP>
+__device__ __forceinline__ void pa_values(PaTile<T, DP>& t, float* s, const unsigned mask, float& m, float& l, pa_f32x4* o) {
+  typedef PaTile<T, DP> Tile;
+  constexpr int NV = Tile::NV;
+  const int g = (threadIdx.x & 63) >> 4;
   constexpr unsigned ALL = Tile::TK == 32 ? 0xffffffffu : 0xffffu;
   if (mask != ALL) {
 #pragma unroll
@@ -191,7 +205,7 @@ __device__ __forceinline__ void pa_tile(PaTile<T, DP>& t, const pa_u32x4* q, con
   mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
   const float mn = fmaxf(m, mt), ref = mn == -INFINITY ? 0.f : mn;
   if (__any(mn > m)) {
-    const float f = exp2f(m - ref);                      // 0 where there was nothing
+    const float f = __builtin_amdgcn_exp2f(m - ref);                      // 0 where there was nothing
     l *= f;
 #pragma unroll
     for (int n = 0; n < Tile::EV; ++n) o[n] *= f;
@@ -199,7 +213,7 @@ __device__ __forceinline__ void pa_tile(PaTile<T, DP>& t, const pa_u32x4* q, con
   }
   float p[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) { p[i] = exp2f(s[i] - ref); l += p[i]; }
+  for (int i = 0; i < NV; ++i) { p[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += p[i]; }
   if constexpr (sizeof(T) == 2) {
     // the rest is never negative, and kept above zero, so that an infinite value keeps its sign: 0 x inf is no number
     pa_u32x4 hi;
@@ -227,10 +241,13 @@ __device__ __forceinline__ void pa_tile(PaTile<T, DP>& t, const pa_u32x4* q, con
 }  // namespace
 
 template <typename T, int DP, bool FULL>
-__global__ __launch_bounds__(64 * PA_WAVES) void paged_attn_kernel(PaArgs p) {
+__global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 ? 3 : 2) void paged_attn_kernel(PaArgs p) {
   typedef PaTile<T, DP> Tile;
   constexpr int TK = Tile::TK, STEPS = Tile::NK / (TK / 16), E = 16 / (int)sizeof(T);
-  __shared__ float s_o[PA_WAVES][PA_ROWS][DP], s_m[PA_WAVES][PA_ROWS], s_l[PA_WAVES][PA_ROWS];
+  constexpr bool Q_LDS = DP == 256;                 // the widest head's query operand takes its registers' place in LDS, under the results
+  __shared__ alignas(16) float s_o[PA_WAVES][PA_ROWS][DP];
+  __shared__ float s_m[PA_WAVES][PA_ROWS], s_l[PA_WAVES][PA_ROWS];
+  pa_u32x4* s_q = (pa_u32x4*)s_o;
   const PagedAttnArgs& a = p.a;
   const int grp = blockIdx.x % p.groups, item = blockIdx.x / p.groups;
   const PaItem it = pa_item(p, item);
@@ -239,53 +256,56 @@ __global__ __launch_bounds__(64 * PA_WAVES) void paged_attn_kernel(PaArgs p) {
   const int hk = grp / p.tiles, qt = grp - hk * p.tiles, per_kv = a.heads_q / a.heads_kv;
   const int h0 = hk * per_kv + qt * PA_ROWS, rows = min(PA_ROWS, per_kv - qt * PA_ROWS);
   const int* row = a.table + (int64_t)it.r * a.pitch;
-  const unsigned ku_page = (unsigned)(a.k_page / E), ku_t = (unsigned)(a.k_t / E), vu_page = (unsigned)(a.v_page / E), vu_t = (unsigned)(a.v_t / E);
+  const PaUnits units = {(unsigned)(a.k_page / E), (unsigned)(a.k_t / E), (unsigned)(a.v_page / E), (unsigned)(a.v_t / E)};
   const char* kb = (const char*)((const T*)a.k + (int64_t)hk * a.k_h);
   const char* vb = (const char*)((const T*)a.v + (int64_t)hk * a.v_h);
 
-  pa_u32x4 q[STEPS];
+  pa_u32x4 q[Q_LDS ? 1 : STEPS];
+  if constexpr (Q_LDS) {
+    for (int s = w; s < STEPS; s += PA_WAVES) s_q[s * 64 + lane] = pa_query<T>(a, it.r, h0, rows, (s * 4 + g) * E);
+    __syncthreads();
+  } else {
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) {
-    const int e = (s * 4 + g) * E;
-    q[s] = pa_u32x4{0, 0, 0, 0};
-    if (c < rows && e < a.d) q[s] = *(const pa_u32x4*)((const T*)a.q + (int64_t)it.r * a.q_r + (int64_t)(h0 + c) * a.q_h + e);
+    for (int s = 0; s < STEPS; ++s) q[s] = pa_query<T>(a, it.r, h0, rows, (s * 4 + g) * E);
   }
   pa_f32x4 o[Tile::EV];
 #pragma unroll
   for (int n = 0; n < Tile::EV; ++n) o[n] = pa_f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  // the wave's tiles: w, w + PA_WAVES, ... of the chunk; places are looked up two tiles ahead, keys and values loaded one ahead
+  // The wave's tiles: w, w + PA_WAVES, ... of the chunk.  The next tile's keys are requested when the logits are done, its values when
+  // the present ones are used up: one set of registers, and something is always on its way.  Loads return in the order of their
+  // issue, so the page table entries are asked for a tile ahead of the loads that need them: waiting for them waits for nothing else.
   constexpr int STEP = TK * PA_WAVES;
-  const int kl = it.k0 + w * TK + (lane & (TK - 1));
-#define PA_WHERE(key) pa_where(a, row, (key), it.k1, ku_page, ku_t, vu_page, vu_t)
-#define PA_MASK(wh) ((unsigned)__ballot((wh).on) & (TK == 32 ? 0xffffffffu : 0xffffu))
   const int tiles = max(0, (it.k1 - it.k0 - w * TK + STEP - 1) / STEP);
   if (tiles > 0) {
-    Tile ta, tb;
-    PaWhere wa = PA_WHERE(kl), wb = PA_WHERE(kl + STEP);
-    pa_load<T, DP, FULL>(ta, wa, kb, vb, a.d);
-    unsigned ma = PA_MASK(wa), mb;
-    for (int i = 0; i < tiles; i += 2) {
-      const int key = kl + i * STEP;
-      pa_load<T, DP, FULL>(tb, wb, kb, vb, a.d);
-      mb = PA_MASK(wb);
-      wa = PA_WHERE(key + 2 * STEP);
+    int key = it.k0 + w * TK + (lane & (TK - 1));
+    Tile t;
+    PaWhere at = pa_where(a, units, row[(unsigned)min(key, it.k1 - 1) / (unsigned)a.page], key, it.k1);
+    int id = row[(unsigned)min(key + STEP, it.k1 - 1) / (unsigned)a.page];
+    pa_load_k<T, DP, FULL>(t, at.k, kb, a.d);
+    __builtin_amdgcn_sched_barrier(0);
+    pa_load_v<T, DP, FULL>(t, at.v, vb, a.d);
+#pragma unroll 1
+    for (int i = 0; i < tiles; ++i) {
+      const unsigned mask = (unsigned)__ballot(at.on) & (TK == 32 ? 0xffffffffu : 0xffffu);
+      float s[Tile::NV];
       __builtin_amdgcn_sched_barrier(0);
-      pa_tile<T, DP>(ta, q, ma, p.scale_log2e, m, l, o);
+      pa_logits<T, DP>(t, [&](int i) { return Q_LDS ? s_q[i * 64 + lane] : q[Q_LDS ? 0 : i]; }, p.scale_log2e, s);
+      key += STEP;
+      at = pa_where(a, units, id, key, it.k1);
+      id = row[(unsigned)min(key + STEP, it.k1 - 1) / (unsigned)a.page];
       __builtin_amdgcn_sched_barrier(0);
-      pa_load<T, DP, FULL>(ta, wa, kb, vb, a.d);
-      ma = PA_MASK(wa);
-      wb = PA_WHERE(key + 3 * STEP);
+      if (i + 1 < tiles) pa_load_k<T, DP, FULL>(t, at.k, kb, a.d);
       __builtin_amdgcn_sched_barrier(0);
-      if (i + 1 < tiles) pa_tile<T, DP>(tb, q, mb, p.scale_log2e, m, l, o);
+      pa_values<T, DP>(t, s, mask, m, l, o);
       __builtin_amdgcn_sched_barrier(0);
+      if (i + 1 < tiles) pa_load_v<T, DP, FULL>(t, at.v, vb, a.d);
     }
   }
-#undef PA_WHERE
-#undef PA_MASK
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  if constexpr (Q_LDS) __syncthreads();
   if (g == 0) { s_m[w][c] = m; s_l[w][c] = l; }
 #pragma unroll
   for (int n = 0; n < Tile::EV; ++n)
@@ -303,13 +323,13 @@ __global__ __launch_bounds__(64 * PA_WAVES) void paged_attn_kernel(PaArgs p) {
     float os = 0.f, ls = 0.f;
 #pragma unroll
     for (int i = 0; i < PA_WAVES; ++i) {
-      const float f = exp2f(s_m[i][r] - ref);
+      const float f = __builtin_amdgcn_exp2f(s_m[i][r] - ref);
       os = fmaf(f, s_o[i][r][e], os);
       ls = fmaf(f, s_l[i][r], ls);
     }
     if (it.n == 1) {
       Elem<T>::st((T*)a.o + (int64_t)it.r * a.o_r + (int64_t)(h0 + r) * a.o_h + e, M == -INFINITY ? 0.f : os / ls);
-      if (a.lse && e == 0) a.lse[(int64_t)it.r * a.heads_q + h0 + r] = M == -INFINITY ? -INFINITY : (M + log2f(ls)) * 0.69314718055994531f;
+      if (a.lse && e == 0) a.lse[(int64_t)it.r * a.heads_q + h0 + r] = M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(ls)) * 0.69314718055994531f;
     } else {
       part[r * a.d + e] = os;
       if (e == 0) { part[p.rows * a.d + 2 * r] = M; part[p.rows * a.d + 2 * r + 1] = ls; }
@@ -345,12 +365,12 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
     float mn = m;
 #pragma unroll
     for (int u = 0; u < U; ++u) mn = fmaxf(mn, mi[u]);
-    const float ref = mn == -INFINITY ? 0.f : mn, f = exp2f(m - ref);
+    const float ref = mn == -INFINITY ? 0.f : mn, f = __builtin_amdgcn_exp2f(m - ref);
     o *= f; l *= f; m = mn;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u * ng >= pl.y) continue;
-      const float fu = exp2f(mi[u] - ref);
+      const float fu = __builtin_amdgcn_exp2f(mi[u] - ref);
       l = fmaf(fu, li[u], l);
 #pragma unroll
       for (int x = 0; x < 4; ++x) o[x] = fmaf(fu, oi[u][x], o[x]);
@@ -365,13 +385,13 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
   for (int i = 0; i < ng; ++i) M = fmaxf(M, s_m[i * lg + e]);
   const float ref = M == -INFINITY ? 0.f : M;
   for (int i = 0; i < ng; ++i) {
-    const float f = exp2f(s_m[i * lg + e] - ref);
+    const float f = __builtin_amdgcn_exp2f(s_m[i * lg + e] - ref);
     L = fmaf(f, s_l[i * lg + e], L);
     for (int x = 0; x < 4; ++x) O[x] = fmaf(f, s_o[i * lg + e][x], O[x]);
   }
   T* out = (T*)a.o + (int64_t)r * a.o_r + (int64_t)h * a.o_h + 4 * e;
   for (int x = 0; x < 4; ++x) Elem<T>::st(out + x, M == -INFINITY ? 0.f : O[x] / L);
-  if (a.lse && e == 0) a.lse[(int64_t)r * a.heads_q + h] = M == -INFINITY ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+  if (a.lse && e == 0) a.lse[(int64_t)r * a.heads_q + h] = M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994531f;
 }
 
 bool paged_attention_fits(int n_req, int heads_q, int heads_kv, int64_t max_keys) {
