@@ -512,8 +512,8 @@ int sm_paged_attention(const sm_paged_attention_desc*, const void* q, const void
  * low four bits; z [N, K / group] bytes 0 .. 15, null: 8 throughout.  group 32, 64 or 128; K a multiple of it; act
  * SM_ACT_NONE or SM_ACT_GELU (erf).  sm_linear_w4_pack writes weights, scales and zero points into `packed`
  * (sm_linear_w4_packed_bytes, caller-owned device memory) in the order the kernel reads them, once.  The products are
- * exact (integers times bf16, fp32 sums); a group's sum takes its scale in fp32.  Made for the rows of a decode step: the
- * weights are streamed once per 32 rows. */
+ * exact (integers times bf16, fp32 sums); a group's sum takes its scale in fp32; a row of x with an infinity or a NaN gives
+ * NaN.  Made for the rows of a decode step: the weights are streamed once per 32 rows. */
 typedef struct { int32_t M, N, K, group, act; } sm_linear_w4_desc;
 size_t sm_linear_w4_packed_bytes(int N, int K, int group);
 int sm_linear_w4_pack(const void* w, const void* scales, const void* zeros, int N, int K, int group, void* packed, void* stream);

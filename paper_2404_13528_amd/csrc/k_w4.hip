@@ -1,15 +1,16 @@
 // Linear with 4-bit weights, group scales and zero points, on few rows: y = act(x W^T + bias) + residual.
 //
-// Bound by the stream of the packed weights (half a byte each, and 4 bytes a group for scale and zero point).  A workgroup
-// takes 16 or 32 output features, its waves take turns over blocks of 128 k and meet in LDS at the end; every weight load of a wave
-// is one contiguous KiB, requested blocks ahead.
+// Bound by the stream of the packed weights (half a byte each, and 4 bytes a group for scale and zero point) and, with many rows, by
+// the x that every workgroup loads (a CU takes in some 45 bytes a ns).  A workgroup has all of K for its 16 to 96 features: its waves
+// take turns over blocks of 128 k and meet in LDS at the end.
 //
-//  * The matrix pipe's first operand is 16 features x 32 k: a lane's 8 k of a feature are one 32-bit word, and its four words
+//  * The matrix pipe's second operand is 16 features x 32 k: a lane's 8 k of a feature are one 32-bit word, and its four words
 //    of a block one 16-byte load.  Nibble j and j + 4 of a word are the k of a pair: (word >> 4 j) & 0x000f000f with
 //    0x4300 in both halves is the pair of bf16 numbers 128 + w, exactly, in at most two instructions.
 //  * The products are integers times bf16 and the sums fp32.  What the offsets 128 + z add, (128 + z) sum of x, is taken off per
-//    group; the sum of x comes from the same instruction with ones as the first operand, so it has the layout of the result.
-//    Then the group's scale is applied, in fp32.
+//    group; the sum of x comes from the same instruction with ones as the second operand, so it has the layout of the result.
+//    Then the group's scale is applied, in fp32.  The rows of the result are the rows of x, a lane's column is one feature:
+//    it needs one word of scale and zero point per group.
 #include <algorithm>
 #include "device_common.h"
 #include "paged.h"
@@ -24,176 +25,242 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 w4_bf16x8;
 constexpr int W4_BLOCK = 128;            // k of a block
 constexpr int W4_WAVES = 8;
 
-struct W4Shape { int tiles, blocks; size_t weights, scales; };       // tiles of 16 features, blocks of k; bytes of either part
-W4Shape w4_shape(int N, int K, int group) {
-  W4Shape s;
-  s.tiles = (N + 15) / 16; s.blocks = (K + W4_BLOCK - 1) / W4_BLOCK;
-  s.weights = (size_t)s.tiles * s.blocks * 1024;
-  s.scales = (size_t)s.tiles * s.blocks * (W4_BLOCK / group) * 64;
-  return s;
-}
+constexpr int w4_record(int groups) { return 1024 + 64 * groups; }      // bytes of a tile's block: weights, then the words of its groups
 
 __device__ __forceinline__ w4_f32x4 w4_mfma(w4_u32x4 a, w4_u32x4 b, w4_f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(w4_bf16x8, a), __builtin_bit_cast(w4_bf16x8, b), c, 0, 0, 0);
 }
-// the eight weights of a word as bf16 128 + w
-__device__ __forceinline__ w4_u32x4 w4_widen(unsigned u) {
+// the eight weights of a word as bf16 128 + w; mask 0x000f000f and offset 0x43004300 are kernel arguments, which the compiler keeps
+// in registers (literals would make two instructions of the and-or)
+__device__ __forceinline__ w4_u32x4 w4_widen(unsigned u, unsigned mask, unsigned offset) {
   w4_u32x4 v;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = ((u >> (4 * j)) & 0x000f000fu) | 0x43004300u;
+  for (int j = 0; j < 4; ++j) v[j] = ((u >> (4 * j)) & mask) | offset;
   return v;
 }
 }  // namespace
 
-size_t w4_packed_bytes(int N, int K, int group) { const W4Shape s = w4_shape(N, K, group); return s.weights + s.scales; }
+size_t w4_packed_bytes(int N, int K, int group) {
+  return (size_t)((N + 15) / 16) * ((K + W4_BLOCK - 1) / W4_BLOCK) * w4_record(W4_BLOCK / group);
+}
 
-// weights: word (tile, block, lane, step) holds k = 128 block + 32 step + 8 (lane / 16) + 0..7 of feature 16 tile + lane % 16, k = 2 j
-// in nibble j and 2 j + 1 in nibble j + 4; scales: word (tile, group, feature) = scale (bf16, upper half) and 128 + zero point (bf16)
+// A record per tile of 16 features and block of 128 k, blocks of a tile one behind the other.  Weights: word (lane, step) holds
+// k = 128 block + 32 step + 8 (lane / 16) + 0..7 of feature 16 tile + lane % 16, k = 2 j in nibble j and 2 j + 1 in nibble j + 4;
+// then word (group, feature) = scale (bf16, upper half) and 128 + zero point (bf16).
 __global__ __launch_bounds__(256) void w4_pack_kernel(const unsigned* w, const bf16_t* s, const unsigned char* z, int N, int K, int group, int blocks,
-                                                      int64_t n_words, int64_t n_scales, unsigned* pw, unsigned* ps) {
+                                                      int64_t n_words, unsigned* packed) {
+  const int words = w4_record(W4_BLOCK / group) / 4, real = K / group;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n_words; i += (int64_t)gridDim.x * 256) {
-    const int step = (int)(i & 3), lane = (int)(i >> 2) & 63;
-    const int64_t tb = i >> 8;
-    const int tile = (int)(tb / blocks), block = (int)(tb - (int64_t)tile * blocks);
-    const int n = tile * 16 + (lane & 15), k = block * W4_BLOCK + step * 32 + (lane >> 4) * 8;
+    const int64_t tb = i / words, tile = tb / blocks;
+    const int at = (int)(i - tb * words), block = (int)(tb - tile * blocks);
     unsigned u = 0;
-    if (n < N && k < K) {
-      const unsigned src = w[((int64_t)n * K + k) / 8];          // nibble e is k + e
+    if (at < 256) {
+      const int step = at & 3, lane = at >> 2, k = block * W4_BLOCK + step * 32 + (lane >> 4) * 8;
+      const int64_t n = tile * 16 + (lane & 15);
+      if (n < N && k < K) {
+        const unsigned src = w[(n * K + k) / 8];                 // nibble e is k + e
 #pragma unroll
-      for (int j = 0; j < 4; ++j) u |= ((src >> (8 * j)) & 15) << (4 * j) | ((src >> (8 * j + 4)) & 15) << (4 * j + 16);
+        for (int j = 0; j < 4; ++j) u |= ((src >> (8 * j)) & 15) << (4 * j) | ((src >> (8 * j + 4)) & 15) << (4 * j + 16);
+      }
+    } else {
+      const int g = block * (W4_BLOCK / group) + (at - 256) / 16;
+      const int64_t n = tile * 16 + (at & 15);
+      if (n < N && g < real) u = (unsigned)s[n * real + g] << 16 | f2bf(128.f + (z ? (float)(z[n * real + g] & 15) : 8.f));
     }
-    pw[i] = u;
-  }
-  const int groups = blocks * (W4_BLOCK / group), real = K / group;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n_scales; i += (int64_t)gridDim.x * 256) {
-    const int64_t tg = i >> 4;
-    const int tile = (int)(tg / groups), g = (int)(tg - (int64_t)tile * groups), n = tile * 16 + (int)(i & 15);
-    unsigned u = 0;
-    if (n < N && g < real) {
-      const int64_t at = (int64_t)n * real + g;
-      u = (unsigned)s[at] << 16 | f2bf(128.f + (z ? (float)(z[at] & 15) : 8.f));
-    }
-    ps[i] = u;
+    packed[i] = u;
   }
 }
 int launch_w4_pack(const void* w, const void* scales, const void* zeros, int N, int K, int group, void* packed, void* stream) {
-  const W4Shape s = w4_shape(N, K, group);
-  const int64_t words = (int64_t)(s.weights / 4);
-  w4_pack_kernel<<<dim3((unsigned)std::min<int64_t>((words + 255) / 256, 4096)), dim3(256), 0, (hipStream_t)stream>>>(
-      (const unsigned*)w, (const bf16_t*)scales, (const unsigned char*)zeros, N, K, group, s.blocks, words, (int64_t)(s.scales / 4), (unsigned*)packed,
-      (unsigned*)((char*)packed + s.weights));
+  const int64_t words = (int64_t)(w4_packed_bytes(N, K, group) / 4);
+  w4_pack_kernel<<<dim3((unsigned)std::min<int64_t>((words + 255) / 256, 8192)), dim3(256), 0, (hipStream_t)stream>>>(
+      (const unsigned*)w, (const bf16_t*)scales, (const unsigned char*)zeros, N, K, group, (K + W4_BLOCK - 1) / W4_BLOCK, words, (unsigned*)packed);
   return (int)hipGetLastError();
 }
 
 namespace {
-struct W4Args { LinearW4Args a; int blocks, tiles; const w4_u32x4* scales; };
+struct W4Args { LinearW4Args a; int blocks, tiles; unsigned mask, offset; };
 
-// what a wave holds of one block of k
-template <int MT, int NT, int GPB> struct W4Block { w4_u32x4 w[NT], s[NT][GPB], x[MT][4]; };
-
-template <int MT, int NT, int GPB>
-__device__ __forceinline__ void w4_load(W4Block<MT, NT, GPB>& b, const W4Args& p, int block, int tile0, const bf16_t* x, int rows) {
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-  if (block >= p.blocks) return;                       // (wave-uniform)
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int64_t tb = (int64_t)min(tile0 + n, p.tiles - 1) * p.blocks + block;
-    b.w[n] = ((const w4_u32x4*)p.a.packed)[tb * 64 + lane];
-#pragma unroll
-    for (int i = 0; i < GPB; ++i) b.s[n][i] = p.scales[(tb * GPB + i) * 4 + g];
-  }
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const int k = block * W4_BLOCK + s * 32 + g * 8;
-      b.x[m][s] = w4_u32x4{0, 0, 0, 0};
-      if (16 * m + c < rows && k < p.a.K) b.x[m][s] = *(const w4_u32x4*)(x + (int64_t)(16 * m + c) * p.a.K + k);
-    }
-}
-template <int MT, int NT, int GPB>
-__device__ __forceinline__ void w4_block(const W4Block<MT, NT, GPB>& b, w4_f32x4 (&tot)[NT][MT]) {
+// One block of one tile: tot += scale (sum over the group of (128 + w) x - (128 + z) sum of x).  keep: 0 takes the block's scales away.
+template <int MT, int GPB>
+__device__ __forceinline__ void w4_block(const w4_u32x4 wv, const unsigned (&sv)[GPB], const w4_u32x4 (&x)[MT][4], w4_f32x4 (&tot)[MT], unsigned mask, unsigned offset,
+                                         unsigned keep) {
   constexpr int STEPS = 4 / GPB;
   const w4_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const w4_u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
   for (int i = 0; i < GPB; ++i) {
-    w4_f32x4 sum[MT], acc[NT][MT];
+    w4_f32x4 sum[MT], acc[MT];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
+      const w4_u32x4 w = w4_widen(wv[i * STEPS + s], mask, offset);
 #pragma unroll
-      for (int m = 0; m < MT; ++m) sum[m] = w4_mfma(ones, b.x[m][i * STEPS + s], s ? sum[m] : zero);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        const w4_u32x4 w = w4_widen(b.w[n][i * STEPS + s]);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[n][m] = w4_mfma(w, b.x[m][i * STEPS + s], s ? acc[n][m] : zero);
+      for (int m = 0; m < MT; ++m) {
+        sum[m] = w4_mfma(x[m][i * STEPS + s], ones, s ? sum[m] : zero);
+        acc[m] = w4_mfma(x[m][i * STEPS + s], w, s ? acc[m] : zero);
       }
     }
+    const float scale = __uint_as_float(sv[i] & keep), off = __uint_as_float(sv[i] << 16);
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float scale = __uint_as_float(b.s[n][i][r] & 0xffff0000u), off = __uint_as_float(b.s[n][i][r] << 16);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) tot[n][m][r] = fmaf(scale, fmaf(-off, sum[m][r], acc[n][m][r]), tot[n][m][r]);
-      }
+      for (int r = 0; r < 4; ++r) tot[m][r] = fmaf(scale, fmaf(-off, sum[m][r], acc[m][r]), tot[m][r]);
   }
+}
+
+__device__ __forceinline__ void w4_store(const LinearW4Args& a, int row, int n, float v) {
+  const int64_t at = (int64_t)row * a.N + n;
+  if (a.bias) v += bf2f(((const bf16_t*)a.bias)[n]);
+  if (a.act) v = gelu_erf(v);
+  if (a.residual) v += bf2f(((const bf16_t*)a.residual)[at]);
+  ((bf16_t*)a.y)[at] = f2bf(v);
 }
 }  // namespace
 
-template <int MT, int NT, int GPB, int PF>
-__global__ __launch_bounds__(64 * W4_WAVES) void w4_kernel(W4Args p) {
-  __shared__ float red[W4_WAVES][NT][MT][16][17];
+// A workgroup has NT tiles of 16 features and MT tiles of 16 rows (HALF: up to 8 rows).  Its waves have PB blocks of k each at a time:
+// a wave's x of these blocks stays in registers while the tiles' weights of the same blocks go by, all of them requested at once (a cold
+// load takes 2 us, so the kernel's time is that of its longest chain of them), the next turn's as the present ones are used up.  The
+// waves' sums of a tile meet in LDS.
+// Loads return in the order of their issue, and the compiler's counting of them survives no branch: all loads are unconditional, and their
+// order is pinned.
+// On the GPU, weights cold: 1 x 4096 x 4096 (groups of 128) 4.2 us, 1 x 22016 x 4096 12.8 us (3.7 TB/s), 32 x 22016 x 4096 18.5 us,
+// 32 x 4096 x 11008 22.8 us (704 KB of x for every workgroup).
+template <int MT, bool HALF, int NT, int GPB, int PB>
+__global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
+  constexpr int RT = NT * MT * W4_WAVES <= 96 ? NT : 96 / MT / W4_WAVES;       // tiles that meet at once
+  __shared__ float red[W4_WAVES][RT][MT][16][17];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * 16 * MT, rows = min(16 * MT, p.a.M - m0);
-  const bf16_t* x = (const bf16_t*)p.a.x + (int64_t)m0 * p.a.K;
+  const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * 16 * MT, rows = min(16 * MT, p.a.M - m0), K = p.a.K;
+  const unsigned mask = p.mask;
+  unsigned offset;
+  asm("v_mov_b32 %0, %1" : "=v"(offset) : "s"(p.offset));      // (an instruction takes one scalar register: the other constant goes to a vector one)
+  const char* xp = (const char*)p.a.x + (int64_t)m0 * K * 2;
+  // rows behind the end read the last one and are not stored
+  unsigned xa[MT], xb[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    xa[m] = (unsigned)min(16 * m + (c & 7), rows - 1) * (unsigned)K;
+    xb[m] = (unsigned)min(16 * m + (c & 7) + 8, rows - 1) * (unsigned)K;
+  }
+  const int k_lane = (c >> 3) * 32 + g * 8;
   w4_f32x4 tot[NT][MT];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int m = 0; m < MT; ++m) tot[n][m] = w4_f32x4{0.f, 0.f, 0.f, 0.f};
-  if (w < p.blocks) {
-    W4Block<MT, NT, GPB> b[PF];
+
+  w4_u32x4 x[PB][MT][4], wv[PB][NT];
+  unsigned sv[PB][NT][GPB];
+  // blocks behind the end read the last one there is, and lose its scales; so do k behind the end, whose scales are zero.
+  // A load of x takes 64 k of 8 rows, eight whole lines of memory: the operand's 32 k of 16 rows would be 16 half ones, and lines are what
+  // loads are counted in.  Two such loads become two operands when lanes 8 .. 15 of a row of lanes change places with lanes 0 .. 7 of the other.
+  auto load_x = [&](int i, int block) {
+    block = min(block, p.blocks - 1);
 #pragma unroll
-    for (int i = 0; i < PF; ++i) w4_load<MT, NT, GPB>(b[i], p, w + i * W4_WAVES, tile0, x, rows);
-    for (int k = w; k < p.blocks; k += PF * W4_WAVES) {
+    for (int s = 0; s < 4; s += 2) {
+      const unsigned k = min(block * W4_BLOCK + s * 32 + k_lane, K - 8);
 #pragma unroll
-      for (int i = 0; i < PF; ++i) {
-        if (k + i * W4_WAVES < p.blocks) w4_block<MT, NT, GPB>(b[i], tot);
-        w4_load<MT, NT, GPB>(b[i], p, k + (i + PF) * W4_WAVES, tile0, x, rows);
+      for (int m = 0; m < MT; ++m) {
+        x[i][m][s] = *(const w4_u32x4*)(xp + 2 * (xa[m] + k));
+        if (!HALF) x[i][m][s + 1] = *(const w4_u32x4*)(xp + 2 * (xb[m] + k));
       }
     }
-  }
-#pragma unroll
-  for (int n = 0; n < NT; ++n)
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto order_x = [&](int i) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) red[w][n][m][c][4 * g + r] = tot[n][m][r];
-  __syncthreads();
-  for (int i = threadIdx.x; i < NT * MT * 256; i += 64 * W4_WAVES) {
-    const int f = i & (16 * NT - 1), row = i / (16 * NT), n = tile0 * 16 + f;
-    if (row >= rows || n >= p.a.N) continue;
-    float v = 0.f;
+      for (int s = 0; s < 4; s += 2)
 #pragma unroll
-    for (int u = 0; u < W4_WAVES; ++u) v += red[u][f >> 4][row >> 4][row & 15][f & 15];
-    const int64_t at = (int64_t)(m0 + row) * p.a.N + n;
-    if (p.a.bias) v += bf2f(((const bf16_t*)p.a.bias)[n]);
-    if (p.a.act) v = gelu_erf(v);
-    if (p.a.residual) v += bf2f(((const bf16_t*)p.a.residual)[at]);
-    ((bf16_t*)p.a.y)[at] = f2bf(v);
+        for (int e = 0; e < 4; ++e) {
+          const int a = x[i][m][s][e], b = HALF ? a : x[i][m][s + 1][e];      // (up to 8 rows: the others are anything)
+          if (!HALF) x[i][m][s][e] = __builtin_amdgcn_update_dpp(a, b, 0x128, 0xf, 0xc, false);
+          x[i][m][s + 1][e] = __builtin_amdgcn_update_dpp(b, a, 0x128, 0xf, 0x3, false);
+        }
+  };
+  auto load_w = [&](int i, int n, int block) {
+    block = min(block, p.blocks - 1);
+    const char* r = (const char*)p.a.packed + ((int64_t)min(tile0 + n, p.tiles - 1) * p.blocks + block) * w4_record(GPB);
+    wv[i][n] = *(const w4_u32x4*)(r + lane * 16);
+#pragma unroll
+    for (int j = 0; j < GPB; ++j) sv[i][n][j] = *(const unsigned*)(r + 1024 + j * 64 + c * 4);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int TURN = W4_WAVES * PB;                  // blocks of a turn: wave w has w * PB ..
+  int block = w * PB;
+  if (block < p.blocks) {
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      load_x(i, block + i);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) load_w(i, n, block + i);
+    }
+#pragma unroll 1
+    for (; block + TURN < p.blocks; block += TURN) {
+#pragma unroll
+      for (int i = 0; i < PB; ++i) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if (n == 0) order_x(i);
+          w4_block<MT, GPB>(wv[i][n], sv[i][n], x[i], tot[n], mask, offset, 0xffff0000u);
+          __builtin_amdgcn_sched_barrier(0);
+          if (n + 1 == NT) load_x(i, block + TURN + i);
+          load_w(i, n, block + TURN + i);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      order_x(i);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) w4_block<MT, GPB>(wv[i][n], sv[i][n], x[i], tot[n], mask, offset, block + i < p.blocks ? 0xffff0000u : 0u);
+    }
+  }
+#pragma unroll
+  for (int n0 = 0; n0 < NT; n0 += RT) {
+    if (n0) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < RT; ++n)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) if (n0 + n < NT) red[w][n][m][4 * g + r][c] = tot[n0 + n < NT ? n0 + n : 0][m][r];
+    __syncthreads();
+    for (int i = threadIdx.x; i < RT * MT * 256; i += 64 * W4_WAVES) {
+      const int f = i % (16 * RT), row = i / (16 * RT), n = (tile0 + n0) * 16 + f;
+      if (row >= rows || n >= p.a.N || n0 + (f >> 4) >= NT) continue;
+      float v = 0.f;
+#pragma unroll
+      for (int u = 0; u < W4_WAVES; ++u) v += red[u][f >> 4][row >> 4][row & 15][f & 15];
+      w4_store(p.a, m0 + row, n, v);
+    }
   }
 }
 
+template <int GPB, int MT, bool HALF, int NT>
+static void w4_go(const W4Args& p, hipStream_t stream) {
+  constexpr int PB = MT == 1 ? 2 : 1;
+  w4_kernel<MT, HALF, NT, GPB, PB><<<dim3((p.tiles + NT - 1) / NT, (p.a.M + 16 * MT - 1) / (16 * MT)), dim3(64 * W4_WAVES), 0, stream>>>(p);
+}
+// Tiles per workgroup, 256 CUs: as many as make the launch one round of workgroups, since every one loads all of x.  Up to 16 rows that is
+// little and three tiles are enough (1 x 22016 x 4096: 12.8 us with 3, 13.5 with 6); beyond, six (32 rows: 18.5 us with 6, 22.1 with 3).
+template <int GPB, int MT, bool HALF>
+static void w4_tiles(const W4Args& p, hipStream_t stream) {
+  const int per_cu = (p.tiles + 255) / 256;
+  if (per_cu <= 1) w4_go<GPB, MT, HALF, 1>(p, stream);
+  else if (per_cu == 2) w4_go<GPB, MT, HALF, 2>(p, stream);
+  else if (per_cu == 3 || MT == 1) w4_go<GPB, MT, HALF, 3>(p, stream);
+  else if (per_cu == 4) w4_go<GPB, MT, HALF, MT == 1 ? 3 : 4>(p, stream);
+  else w4_go<GPB, MT, HALF, MT == 1 ? 3 : 6>(p, stream);
+}
 template <int GPB>
 static void w4_launch(const W4Args& p, hipStream_t stream) {
-  if (p.a.M <= 16) w4_kernel<1, 1, GPB, 4><<<dim3(p.tiles), dim3(64 * W4_WAVES), 0, stream>>>(p);
-  else w4_kernel<2, 2, GPB, 2><<<dim3((p.tiles + 1) / 2, (p.a.M + 31) / 32), dim3(64 * W4_WAVES), 0, stream>>>(p);
+  if (p.a.M <= 8) w4_tiles<GPB, 1, true>(p, stream);
+  else if (p.a.M <= 16) w4_tiles<GPB, 1, false>(p, stream);
+  else w4_tiles<GPB, 2, false>(p, stream);
 }
 int launch_w4(const LinearW4Args& a, void* stream) {
-  const W4Shape s = w4_shape(a.N, a.K, a.group);
-  const W4Args p{a, s.blocks, s.tiles, (const w4_u32x4*)((const char*)a.packed + s.weights)};
+  const W4Args p{a, (a.K + W4_BLOCK - 1) / W4_BLOCK, (a.N + 15) / 16, 0x000f000fu, 0x43004300u};
   if (a.group == 128) w4_launch<1>(p, (hipStream_t)stream);
   else if (a.group == 64) w4_launch<2>(p, (hipStream_t)stream);
   else w4_launch<4>(p, (hipStream_t)stream);
