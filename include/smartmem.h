@@ -473,7 +473,7 @@ int sm_page_table(const sm_page_cfg*, const int32_t* cached, const int32_t* fres
  * (with its output): that part is left out.  Strides: token, head for inputs and q_out; page, token, head for k_out and
  * v_out.  slots null: row t of k_out / v_out is t * stride[1] + head * stride[2].  slots given: k_out / v_out are page
  * pools and row t goes to page slots[t] / page, place slots[t] % page; a slot outside [0, n_pages * page) stores nothing.
- * A token with a negative position is padding: nothing of it is read or written.  Two tokens of one slot: each head of
+ * A token with a negative position is padding: nothing is stored for it.  Two tokens of one slot: each head of
  * the slot holds either of them.  An output may be its input (same address and strides), otherwise they must not overlap.
  * Angles are exact to a 2^-31 revolution at any position.  rot a multiple of twice the 16-byte vector (16 bf16, 8 f32),
  * d a multiple of the vector, both at most 256; rope_base >= 1; n_pages * page <= 2^30. */

@@ -1,11 +1,12 @@
 // Norm of every query / key head, rotary embedding, and the store of queries, keys and values where the attention reads
 // them (a page pool or plain rows), one pass over the fused projection's result.
 //
-// A head of d features lies over G lanes of 16 bytes; a wave takes 64 / G heads of one token at a time, and the workgroup's
-// waves share the heads of a token.  An element's rotation partner is in the same wave, rot / 2 features away.
+// A lane has two 16-byte pieces of a head: below `rot` the two halves of its pairs, so that the rotation stays in the lane and an angle
+// serves both, behind it two adjacent pieces.  G lanes make a head, a wave takes 64 / G heads of one token at a time.
 // Angles: position times theta_i / 2 pi as a fraction of 2^64, modulo one revolution, is an integer product, exact at any
 // position; its upper 32 bits go to the sine and cosine (bf16: the hardware's, whose 1e-6 is far below the rounding of the
 // store; fp32: the library's, in units of pi).
+// Bound by the bytes read and written.
 #include "device_common.h"
 #include "paged.h"
 
@@ -37,89 +38,144 @@ __device__ __forceinline__ void hn_sincos(uint64_t turn, unsigned pos, float* sn
 }
 }  // namespace
 
-template <typename T, int G>
+// sum over groups of G adjacent lanes, in all of them
+template <int G>
+__device__ __forceinline__ float hn_sum(float v) {
+#define HN_DPP(c) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), c, 0xf, 0xf, true))
+  HN_DPP(0xb1);                                        // quad_perm 1 0 3 2
+  HN_DPP(0x4e);                                        // quad_perm 2 3 0 1
+  if (G >= 8) HN_DPP(0x141);                           // row_half_mirror: the other four of eight
+  if (G >= 16) HN_DPP(0x128);                          // row_ror 8: the other eight of sixteen
+#undef HN_DPP
+  if (G >= 32) v += __shfl_xor(v, 16, 64);
+  return v;
+}
+
+// WPT waves share a token.  A wave's heads (of q, then k, then v: `units` of 64 / G) are requested one unit ahead of the work; position,
+// slot, gains and the first heads are all on their way at the same time.
+template <typename T, int G, int WPT>
 __global__ __launch_bounds__(256) void head_norm_rope_kernel(HeadNormArgs a_) {
   const SM_KARG HeadNormArgs* a = kernarg_ptr<HeadNormArgs>();
   constexpr int V = Elem<T>::VEC, HPW = 64 / G;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, t = blockIdx.x;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t t = WPT == 1 ? (int64_t)blockIdx.x * 4 + w : blockIdx.x;
+  if (t >= a->tokens) return;
+  const int l = lane & (G - 1), sub = lane / G, hv = a->rot / (2 * V), dv = a->d / V, norm = a->norm;
+  const bool turns = l < hv;
+  const int i0 = turns ? l : 2 * l, i1 = turns ? l + hv : i0 + 1;      // (behind rot: piece rot / V + 2 (l - hv) and the next)
+  const bool on0 = i0 < dv, on1 = i1 < dv;
+  const int n0 = a->part[0].units, n1 = n0 + a->part[1].units, n2 = n1 + a->part[2].units;
+  auto load = [&](int u, hn_u32x4& x0, hn_u32x4& x1) {
+    const int p = u < n0 ? 0 : u < n1 ? 1 : 2;
+    const T* x = (const T*)(p == 0 ? a->part[0].x : p == 1 ? a->part[1].x : a->part[2].x);
+    const int64_t xt = p == 0 ? a->part[0].x_t : p == 1 ? a->part[1].x_t : a->part[2].x_t, xh = p == 0 ? a->part[0].x_h : p == 1 ? a->part[1].x_h : a->part[2].x_h;
+    const int heads = p == 0 ? a->part[0].heads : a->part[p].heads, h = (u - (p == 0 ? 0 : p == 1 ? n0 : n1)) * HPW + sub;
+    x0 = x1 = hn_u32x4{0, 0, 0, 0};
+    if (u < n2 && h < heads) {
+      x += t * xt + h * xh;
+      if (on0) x0 = *(const hn_u32x4*)(x + i0 * V);
+      if (on1) x1 = *(const hn_u32x4*)(x + i1 * V);
+    }
+  };
+  int u = WPT == 1 ? 0 : w;
+  if (u >= n2) return;
+  hn_u32x4 x0, x1, gain[2][2], shift[2][2];
+  load(u, x0, x1);
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const T *g = (const T*)a->part[p].gamma, *b = (const T*)a->part[p].beta;
+    gain[p][0] = gain[p][1] = shift[p][0] = shift[p][1] = hn_u32x4{0, 0, 0, 0};
+    if (norm && a->part[p].units) {
+      if (on0) gain[p][0] = *(const hn_u32x4*)(g + i0 * V);
+      if (on1) gain[p][1] = *(const hn_u32x4*)(g + i1 * V);
+      if (norm == 1 && on0) shift[p][0] = *(const hn_u32x4*)(b + i0 * V);
+      if (norm == 1 && on1) shift[p][1] = *(const hn_u32x4*)(b + i1 * V);
+    }
+  }
   const int pos = a->positions[t];
+  const int slot = a->slots ? a->slots[t] : 0;
   if (pos < 0) return;
-  const int e0 = (lane & (G - 1)) * V, sub = lane / G, half = a->rot / 2, d = a->d;
-  const bool in = e0 < d, turns = e0 < a->rot, low = e0 < half;
-  const int partner = low ? lane + half / V : lane - half / V;
+  const bool store = !a->slots || (slot >= 0 && slot < a->n_slots);
+  const int page = a->slots && store ? slot / a->page : 0;
+  const int64_t row = a->slots ? slot - page * a->page : t;
   float sn[V], cs[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) { sn[e] = 0.f; cs[e] = 1.f; }
   if (turns) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      hn_sincos<T>(a->turn[(low ? e0 : e0 - half) + e], (unsigned)pos, &sn[e], &cs[e]);
-      if (low) sn[e] = -sn[e];
-    }
+    for (int e = 0; e < V; ++e) hn_sincos<T>(a->turn[l * V + e], (unsigned)pos, &sn[e], &cs[e]);
   }
-  int64_t slot = t, page = 0;
-  bool store = true;
-  if (a->slots) {
-    slot = a->slots[t];
-    store = slot >= 0 && slot < a->n_slots;
-    page = store ? (int)slot / a->page : 0;
-    slot -= page * a->page;
-  }
-  int u = w;
-  for (int p = 0; p < 3; ++p) {
-    const SM_KARG HeadNormPart* q = &a->part[p];
-    for (; u < q->units; u += 4) {
-      const int h = u * HPW + sub;
-      const bool on = in && h < q->heads;
-      hn_u32x4 x = {0, 0, 0, 0};
-      if (on) x = *(const hn_u32x4*)((const T*)q->x + t * q->x_t + h * q->x_h + e0);
-      if (q->rotate) {
-        float f[V];
-        hn_unpack<T>(x, f);
-        if (a->norm) {
-          float mean = 0.f, sq = 0.f;
-          if (a->norm == 1) {
+  const float inv_d = 1.f / a->d, eps = a->eps;
+  auto work = [&](const hn_u32x4 (&gv)[2], const hn_u32x4 (&bv)[2]) {
+    float f0[V], f1[V];
+    hn_unpack<T>(x0, f0);
+    hn_unpack<T>(x1, f1);
+    if (norm) {
+      float sq = 0.f, g0[V], g1[V], b0[V], b1[V];
+      if (norm == 1) {
+        float mean = 0.f;
 #pragma unroll
-            for (int e = 0; e < V; ++e) mean += f[e];
+        for (int e = 0; e < V; ++e) mean += f0[e] + f1[e];
+        mean = hn_sum<G>(mean) * inv_d;
 #pragma unroll
-            for (int o = 1; o < G; o <<= 1) mean += __shfl_xor(mean, o, 64);
-            mean /= d;
-          }
-#pragma unroll
-          for (int e = 0; e < V; ++e) { f[e] = in ? f[e] - mean : 0.f; sq = fmaf(f[e], f[e], sq); }
-#pragma unroll
-          for (int o = 1; o < G; o <<= 1) sq += __shfl_xor(sq, o, 64);
-          const float r = 1.f / sqrtf(sq / d + a->eps);
-          float g[V], b[V];
-          hn_u32x4 gv = {0, 0, 0, 0}, bv = {0, 0, 0, 0};
-          if (in) gv = *(const hn_u32x4*)((const T*)q->gamma + e0);
-          if (in && a->norm == 1) bv = *(const hn_u32x4*)((const T*)q->beta + e0);
-          hn_unpack<T>(gv, g);
-          hn_unpack<T>(bv, b);
-#pragma unroll
-          for (int e = 0; e < V; ++e) f[e] = fmaf(f[e] * r, g[e], b[e]);
-        }
-        if (half) {
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float o = __shfl(f[e], partner & 63, 64);
-            if (turns) f[e] = fmaf(o, sn[e], f[e] * cs[e]);
-          }
-        }
-        x = hn_pack<T>(f);
+        for (int e = 0; e < V; ++e) { f0[e] = on0 ? f0[e] - mean : 0.f; f1[e] = on1 ? f1[e] - mean : 0.f; }
       }
-      const int64_t off = q->paged ? page * q->y_page + slot * q->y_t : t * q->y_t;
-      if (on && (store || !q->paged)) *(hn_u32x4*)((T*)q->y + off + h * q->y_h + e0) = x;
+#pragma unroll
+      for (int e = 0; e < V; ++e) { sq = fmaf(f0[e], f0[e], sq); sq = fmaf(f1[e], f1[e], sq); }
+      const float r = rsqrtf(fmaf(hn_sum<G>(sq), inv_d, eps));
+      hn_unpack<T>(gv[0], g0);
+      hn_unpack<T>(gv[1], g1);
+      hn_unpack<T>(bv[0], b0);
+      hn_unpack<T>(bv[1], b1);
+#pragma unroll
+      for (int e = 0; e < V; ++e) { f0[e] = fmaf(f0[e] * r, g0[e], b0[e]); f1[e] = fmaf(f1[e] * r, g1[e], b1[e]); }
     }
-    u -= q->units;
+    if (hv) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float lo = f0[e], hi = f1[e];
+        f0[e] = fmaf(-hi, sn[e], lo * cs[e]);
+        f1[e] = fmaf(lo, sn[e], hi * cs[e]);
+      }
+    }
+    x0 = hn_pack<T>(f0);
+    x1 = hn_pack<T>(f1);
+  };
+  for (; u < n2; u += WPT) {
+    hn_u32x4 y0, y1;
+    load(u + WPT, y0, y1);
+    const int p = u < n0 ? 0 : u < n1 ? 1 : 2, h = (u - (p == 0 ? 0 : p == 1 ? n0 : n1)) * HPW + sub;
+    if (p == 0) work(gain[0], shift[0]);
+    else if (p == 1) work(gain[1], shift[1]);
+    const SM_KARG HeadNormPart* q = &a->part[p];
+    if (h < q->heads && (store || !q->paged)) {
+      T* y = (T*)q->y + h * q->y_h + (q->paged ? page * q->y_page + row * q->y_t : t * q->y_t);
+      // (a long prompt's result is larger than the L2 when its reader starts)
+      auto put = [](T* at, hn_u32x4 v) { if (WPT == 1) __builtin_nontemporal_store(v, (hn_u32x4*)at); else *(hn_u32x4*)at = v; };
+      if (on0) put(y + i0 * V, x0);
+      if (on1) put(y + i1 * V, x1);
+    }
+    x0 = y0;
+    x1 = y1;
   }
 }
 
+// Few tokens: four waves share one (8 tokens of 32 + 8 + 8 heads of 128: 4.7 us instead of 7.9; 512 tokens: 7.3 instead of 9.3).  Once there is
+// a token for most of the 1024 SIMDs, one wave has all heads of a token and the angles are computed once (1024 tokens: 9.7 us instead of
+// 11.2; 16411: 82 instead of 121, 4.9 TB/s read and written, the rate of a large copy).
+template <typename T, int G>
+static void launch_head_norm_g(HeadNormArgs& a, hipStream_t stream) {
+  for (auto& p : a.part) p.units = (p.heads + 64 / G - 1) / (64 / G);
+  if (a.tokens < 768) head_norm_rope_kernel<T, G, 4><<<dim3(a.tokens), dim3(256), 0, stream>>>(a);
+  else head_norm_rope_kernel<T, G, 1><<<dim3((a.tokens + 3) / 4), dim3(256), 0, stream>>>(a);
+}
 template <typename T>
 static int launch_head_norm_t(HeadNormArgs& a, hipStream_t stream) {
-  const int lanes = a.d / Elem<T>::VEC;
-#define SM_HN(G) { for (auto& p : a.part) p.units = (p.heads + 64 / G - 1) / (64 / G); \
-    head_norm_rope_kernel<T, G><<<dim3(a.tokens), dim3(256), 0, stream>>>(a); }
-  if (lanes <= 8) SM_HN(8) else if (lanes <= 16) SM_HN(16) else if (lanes <= 32) SM_HN(32) else SM_HN(64)
-#undef SM_HN
+  const int lanes = (a.d / Elem<T>::VEC + 1) / 2;
+  if (lanes <= 4) launch_head_norm_g<T, 4>(a, stream);
+  else if (lanes <= 8) launch_head_norm_g<T, 8>(a, stream);
+  else if (lanes <= 16) launch_head_norm_g<T, 16>(a, stream);
+  else launch_head_norm_g<T, 32>(a, stream);
   return (int)hipGetLastError();
 }
 int launch_head_norm_rope(HeadNormArgs& a, int dtype, void* stream) {

@@ -2,8 +2,8 @@
 //
 // Bound by the stream of K and V from HBM (4 d bytes and, with g query heads to a key head, 4 g d operations per token and key
 // head in bf16).  Work is cut by the lengths that the device finds: all requests' tokens are divided into chunks of one
-// length, such that about PA_ITEMS workgroups have one each, whatever the mix of short and long requests; every wave finds
-// its workgroup's chunk with one scan over the lengths.  Chunks of a request are joined by a second, small kernel.
+// length, such that a workgroup has one, whatever the mix of short and long requests; every wave finds its workgroup's chunk
+// with two scans over the lengths.  Chunks of a request are joined by a second, small kernel.
 //
 //  * A wave takes tiles of 32 (bf16) or 16 (fp32) keys straight from memory into registers, the next keys and values requested
 //    as soon as the present ones are used up; there is no LDS on the way and no barrier in the loop.
@@ -29,58 +29,86 @@ typedef unsigned int pa_u32x2 __attribute__((ext_vector_type(2)));
 typedef float pa_f32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 pa_bf16x8;
 
-constexpr int PA_WAVES = 4;
-constexpr int PA_ITEMS = 1024;            // workgroups that the work is cut for
-constexpr int PA_CHUNK = 256;             // no chunk shorter than this
 constexpr int PA_ROWS = 16;               // query heads a workgroup serves at once
+constexpr int PA_UNIT = 128;              // keys: chunks are whole units
 
-struct PaShape { int rows, tiles, groups, items; };      // query heads per tile, tiles per key head, workgroups per chunk, chunks at most
-PaShape pa_shape(int n_req, int heads_q, int heads_kv, int64_t max_keys) {
+// How the work is cut.  A chunk's start costs some 5 us (lengths, page table, first keys: three trips to memory), so a chunk is as long as
+// lets all workgroups be resident at once; but where that makes it longer than 512 KB of keys and values, up to 4096 shorter ones balance
+// the load better than they cost (64 requests of 100 to 30000 keys: 272 us instead of 288; one request of 131071 keys is best off
+// with the 1024 that fit).
+constexpr int PA_MANY_LOG2 = 12;
+struct PaShape {
+  int rows, tiles, groups;                // query heads per tile, tiles per key head, workgroups per chunk
+  int fill_log2, cap, least;              // workgroups that fit, units of a long and of the shortest chunk
+  int items;                              // chunks at most
+};
+PaShape pa_shape(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t max_keys) {
   PaShape s;
   const int g = heads_q / heads_kv;
   s.rows = std::min(g, PA_ROWS);
   s.tiles = (g + PA_ROWS - 1) / PA_ROWS;
   s.groups = heads_kv * s.tiles;
-  const int64_t most = (int64_t)n_req * ((max_keys + PA_CHUNK - 1) / PA_CHUNK);
-  s.items = (int)std::min<int64_t>(std::max(1, PA_ITEMS / s.groups) + n_req, most);
+  s.fill_log2 = d > 128 ? 9 : 10;
+  s.cap = std::max(1, (512 << 10) / (2 * d * (dtype == 0 ? 4 : 2) * PA_UNIT));
+  s.least = max_keys <= 2 * PA_UNIT ? 2 : 1;          // (256 keys are one workgroup's, without a join)
+  const int64_t units = (max_keys + PA_UNIT - 1) / PA_UNIT, share = (n_req * units * s.groups + (1 << s.fill_log2) - 1) >> s.fill_log2;
+  const int64_t most = n_req * ((units + s.least - 1) / s.least);
+  s.items = (int)std::min<int64_t>(((1 << (share <= s.cap ? s.fill_log2 : PA_MANY_LOG2)) / s.groups) + n_req, most);
   return s;
 }
 // floats of a workgroup's partial result: [rows][d] sums, [rows][2] maximum and sum of the weights
 __host__ __device__ constexpr int pa_record(int rows, int d) { return (rows * (d + 2) + 3) & ~3; }
 constexpr size_t pa_align(size_t n) { return (n + 255) & ~(size_t)255; }
 
-struct PaArgs { PagedAttnArgs a; int rows, tiles, groups, items; float scale_log2e; int2* plan; };
+struct PaArgs { PagedAttnArgs a; PaShape s; float scale_log2e; int2* plan; };
 
-// The chunk of workgroup `item`: request, first key, one behind the last key, number of the request's chunks.
+// sum over the lanes up to and including this one
+__device__ __forceinline__ unsigned pa_scan(unsigned x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8: within rows of 16 lanes
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // row_bcast 15, 31: the rows before
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
+// The chunk of workgroup `item`: request (-1: none), first key, one behind the last key, number of the request's chunks.
+// A lane has `per` requests.  With U units in all, `share` = U groups / 2^fill units would fill the chip; every request has at least one
+// chunk, so chunks of at least that length are at most 2^fill / groups + n_req.
 struct PaItem { int r, k0, k1, n; };
 __device__ __forceinline__ int pa_len(const PagedAttnArgs& a, int r) { return min(max(a.lens[r], 0), a.max_pages * a.page); }
-__device__ __forceinline__ PaItem pa_item(const PaArgs& p, const int item) {
+__device__ __forceinline__ unsigned pa_chunks(int len, unsigned chunk) { return max(1u, ((unsigned)(len + PA_UNIT - 1) / PA_UNIT + chunk - 1) / chunk); }
+__device__ __forceinline__ PaItem pa_item(const PaArgs& p, const unsigned item) {
   const int lane = threadIdx.x & 63, R = p.a.n_req, per = (R + 63) / 64;
   const int r0 = min(R, lane * per), r1 = min(R, r0 + per);
-  int64_t total = 0;
-  for (int r = r0; r < r1; ++r) total += pa_len(p.a, r);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o, 64);
-  const int64_t share = (total * p.groups + PA_ITEMS - 1) / PA_ITEMS;
-  const int chunk = max(PA_CHUNK, (int)min((share + 127) & ~(int64_t)127, (int64_t)1 << 30));
-  int mine = 0;
-  for (int r = r0; r < r1; ++r) mine += max(1, (pa_len(p.a, r) + chunk - 1) / chunk);
-  int end = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(end, o, 64); if (lane >= o) end += u; }
+  const int len0 = r0 < r1 ? pa_len(p.a, r0) : 0;      // (of a lane's first request; up to 64 requests need no other)
+  unsigned mine = (unsigned)(len0 + PA_UNIT - 1) / PA_UNIT;
+  for (int r = r0 + 1; r < r1; ++r) mine += (unsigned)(pa_len(p.a, r) + PA_UNIT - 1) / PA_UNIT;
+  // (a lane's units fit 32 bits, their sum over the lanes is taken in two halves)
+  const uint64_t units = (uint64_t)__builtin_amdgcn_readlane(pa_scan(mine & 0xffffu), 63) + ((uint64_t)__builtin_amdgcn_readlane(pa_scan(mine >> 16), 63) << 16);
+  const uint64_t total = units * (unsigned)p.s.groups;
+  const uint64_t share = (total + (1u << p.s.fill_log2) - 1) >> p.s.fill_log2, many = (total + (1u << PA_MANY_LOG2) - 1) >> PA_MANY_LOG2;
+  const uint64_t want = share <= (uint64_t)p.s.cap ? share : max((uint64_t)p.s.cap, many);
+  const unsigned chunk = max((unsigned)p.s.least, (unsigned)min(want, (uint64_t)1 << 23));
+  mine = r0 < r1 ? pa_chunks(len0, chunk) : 0;
+  for (int r = r0 + 1; r < r1; ++r) mine += pa_chunks(pa_len(p.a, r), chunk);
+  const unsigned end = pa_scan(mine);
   PaItem it = {-1, 0, 0, 0};
   const uint64_t holds = __ballot(item < end);
   if (!holds) return it;
   const int src = __builtin_ctzll(holds);
-  int first = __shfl(end - mine, src, 64), r = src * per;
-  for (;; ++r) {                                       // (ends: the lane's requests have the item)
-    const int len = pa_len(p.a, r), n = max(1, (len + chunk - 1) / chunk);
+  unsigned first = __builtin_amdgcn_readlane(end, src) - __builtin_amdgcn_readlane(mine, src);
+  int r = src * per, len = __builtin_amdgcn_readlane(len0, src);
+  for (;;) {                                           // (ends: the lane's requests have the item)
+    const unsigned n = pa_chunks(len, chunk);
     if (item < first + n) {
-      const int64_t k0 = (int64_t)(item - first) * chunk;
-      it = {r, (int)k0, (int)min(k0 + chunk, (int64_t)len), n};
+      const int64_t k0 = (int64_t)(item - first) * chunk * PA_UNIT;
+      it = {r, (int)k0, (int)min(k0 + (int64_t)chunk * PA_UNIT, (int64_t)len), (int)n};
       break;
     }
     first += n;
+    len = pa_len(p.a, ++r);
   }
   it.r = __builtin_amdgcn_readfirstlane(it.r); it.k0 = __builtin_amdgcn_readfirstlane(it.k0);
   it.k1 = __builtin_amdgcn_readfirstlane(it.k1); it.n = __builtin_amdgcn_readfirstlane(it.n);
@@ -240,8 +268,8 @@ __device__ __forceinline__ void pa_values(PaTile<T, DP>& t, float* s, const unsi
 }
 }  // namespace
 
-template <typename T, int DP, bool FULL>
-__global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 ? 3 : 2) void paged_attn_kernel(PaArgs p) {
+template <typename T, int DP, bool FULL, int PA_WAVES>
+__global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 && PA_WAVES == 4 ? 3 : 2) void paged_attn_kernel(PaArgs p) {
   typedef PaTile<T, DP> Tile;
   constexpr int TK = Tile::TK, STEPS = Tile::NK / (TK / 16), E = 16 / (int)sizeof(T);
   constexpr bool Q_LDS = DP == 256;                 // the widest head's query operand takes its registers' place in LDS, under the results
@@ -249,11 +277,11 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 ? 3 : 2) vo
   __shared__ float s_m[PA_WAVES][PA_ROWS], s_l[PA_WAVES][PA_ROWS];
   pa_u32x4* s_q = (pa_u32x4*)s_o;
   const PagedAttnArgs& a = p.a;
-  const int grp = blockIdx.x % p.groups, item = blockIdx.x / p.groups;
+  const int grp = blockIdx.x % p.s.groups, item = blockIdx.x / p.s.groups;
   const PaItem it = pa_item(p, item);
   if (it.r < 0) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int hk = grp / p.tiles, qt = grp - hk * p.tiles, per_kv = a.heads_q / a.heads_kv;
+  const int hk = grp / p.s.tiles, qt = grp - hk * p.s.tiles, per_kv = a.heads_q / a.heads_kv;
   const int h0 = hk * per_kv + qt * PA_ROWS, rows = min(PA_ROWS, per_kv - qt * PA_ROWS);
   const int* row = a.table + (int64_t)it.r * a.pitch;
   const PaUnits units = {(unsigned)(a.k_page / E), (unsigned)(a.k_t / E), (unsigned)(a.v_page / E), (unsigned)(a.v_t / E)};
@@ -312,7 +340,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 ? 3 : 2) vo
 #pragma unroll
     for (int i = 0; i < 4; ++i) s_o[w][c][(4 * g + i) * Tile::EV + n] = o[n][i];
   __syncthreads();
-  float* part = a.part + ((int64_t)item * p.groups + grp) * pa_record(p.rows, a.d);
+  float* part = a.part + ((int64_t)item * p.s.groups + grp) * pa_record(p.s.rows, a.d);
   if (grp == 0 && it.k0 == 0 && threadIdx.x == 0) p.plan[it.r] = make_int2(item, it.n);
   for (int x = threadIdx.x; x < rows * a.d; x += 64 * PA_WAVES) {
     const int r = x / a.d, e = x - r * a.d;
@@ -332,7 +360,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 ? 3 : 2) vo
       if (a.lse && e == 0) a.lse[(int64_t)it.r * a.heads_q + h0 + r] = M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(ls)) * 0.69314718055994531f;
     } else {
       part[r * a.d + e] = os;
-      if (e == 0) { part[p.rows * a.d + 2 * r] = M; part[p.rows * a.d + 2 * r + 1] = ls; }
+      if (e == 0) { part[p.s.rows * a.d + 2 * r] = M; part[p.s.rows * a.d + 2 * r + 1] = ls; }
     }
   }
 }
@@ -347,8 +375,8 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
   if (pl.y <= 1) return;
   const int per_kv = a.heads_q / a.heads_kv, hk = h / per_kv, hr = h - hk * per_kv, qt = hr / PA_ROWS, row = hr - qt * PA_ROWS;
   const int d4 = a.d / 4, lg = d4 <= 16 ? 16 : (d4 <= 32 ? 32 : 64), ng = 256 / lg, e = threadIdx.x & (lg - 1), grp = threadIdx.x / lg;
-  const int64_t rec = (int64_t)p.groups * pa_record(p.rows, a.d);
-  const float* base = a.part + ((int64_t)pl.x * p.groups + hk * p.tiles + qt) * pa_record(p.rows, a.d);
+  const int64_t rec = (int64_t)p.s.groups * pa_record(p.s.rows, a.d);
+  const float* base = a.part + ((int64_t)pl.x * p.s.groups + hk * p.s.tiles + qt) * pa_record(p.s.rows, a.d);
   float m = -INFINITY, l = 0.f;
   pa_f32x4 o = {0.f, 0.f, 0.f, 0.f};
   constexpr int U = 8;
@@ -358,7 +386,7 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const float* q = base + (int64_t)min(i0 + u * ng, pl.y - 1) * rec;
-      const float2 ml = *(const float2*)(q + p.rows * a.d + 2 * row);
+      const float2 ml = *(const float2*)(q + p.s.rows * a.d + 2 * row);
       mi[u] = i0 + u * ng < pl.y ? ml.x : -INFINITY; li[u] = ml.y;
       oi[u] = e < d4 ? *(const pa_f32x4*)(q + row * a.d + 4 * e) : pa_f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -394,20 +422,26 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
   if (a.lse && e == 0) a.lse[(int64_t)r * a.heads_q + h] = M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994531f;
 }
 
-bool paged_attention_fits(int n_req, int heads_q, int heads_kv, int64_t max_keys) {
-  const PaShape s = pa_shape(n_req, heads_q, heads_kv, max_keys);
-  return (int64_t)s.items * s.groups < (1 << 24);      // a launch has less than 2^32 threads
+bool paged_attention_fits(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t max_keys) {
+  const PaShape s = pa_shape(dtype, n_req, heads_q, heads_kv, d, max_keys);
+  // a launch has less than 2^32 threads, and a lane's share of the requests less than 2^32 units
+  return (int64_t)s.items * s.groups < (1 << 23) && (int64_t)((n_req + 63) / 64) * ((max_keys + PA_UNIT - 1) / PA_UNIT) < ((int64_t)1 << 32);
 }
-size_t paged_attention_workspace(int, int n_req, int heads_q, int heads_kv, int d, int page, int max_pages) {
-  const PaShape s = pa_shape(n_req, heads_q, heads_kv, (int64_t)page * max_pages);
+size_t paged_attention_workspace(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t max_keys) {
+  const PaShape s = pa_shape(dtype, n_req, heads_q, heads_kv, d, max_keys);
   return pa_align((size_t)std::max(1, n_req) * sizeof(int2)) + pa_align((size_t)s.items * s.groups * pa_record(s.rows, d) * sizeof(float));
 }
 
+// Requests of at most 256 keys have one workgroup each: eight waves finish its eight tiles at once, and nothing is joined.
 template <typename T, int DP, bool FULL>
 static int pa_launch(const PaArgs& p, bool join, hipStream_t stream) {
-  paged_attn_kernel<T, DP, FULL><<<dim3(p.items * p.groups), dim3(64 * PA_WAVES), 0, stream>>>(p);
+  if (!join) {
+    paged_attn_kernel<T, DP, FULL, 8><<<dim3(p.s.items * p.s.groups), dim3(512), 0, stream>>>(p);
+    return (int)hipGetLastError();
+  }
+  paged_attn_kernel<T, DP, FULL, 4><<<dim3(p.s.items * p.s.groups), dim3(256), 0, stream>>>(p);
   if (const int e = (int)hipGetLastError()) return e;
-  if (join) paged_attn_join_kernel<T><<<dim3(p.a.heads_q, p.a.n_req), dim3(256), 0, stream>>>(p);
+  paged_attn_join_kernel<T><<<dim3(p.a.heads_q, p.a.n_req), dim3(256), 0, stream>>>(p);
   return (int)hipGetLastError();
 }
 template <typename T>
@@ -423,10 +457,9 @@ static int pa_launch_d(const PaArgs& p, bool join, hipStream_t stream) {
 
 int launch_paged_attention(const PagedAttnArgs& a, int dtype, void* stream, int* launches) {
   const int64_t max_keys = (int64_t)a.page * a.max_pages;
-  const PaShape s = pa_shape(a.n_req, a.heads_q, a.heads_kv, max_keys);
-  PaArgs p{a, s.rows, s.tiles, s.groups, s.items, a.scale * 1.4426950408889634f, (int2*)a.part};
+  PaArgs p{a, pa_shape(dtype, a.n_req, a.heads_q, a.heads_kv, a.d, max_keys), a.scale * 1.4426950408889634f, (int2*)a.part};
   p.a.part = (float*)((char*)a.part + pa_align((size_t)a.n_req * sizeof(int2)));
-  const bool join = max_keys > PA_CHUNK;               // else no request has two chunks
+  const bool join = max_keys > p.s.least * PA_UNIT;    // else no request has two chunks
   *launches = join ? 2 : 1;
   return dtype == 0 ? pa_launch_d<float>(p, join, (hipStream_t)stream) : pa_launch_d<bf16_t>(p, join, (hipStream_t)stream);
 }

@@ -110,14 +110,14 @@ int check_paged_attention(const sm_paged_attention_desc* c, const char* who) {
     return fail(SM_ERR_SHAPE, "%s: strides must keep 16-byte alignment", who);
   const int64_t last[2] = {pool_units(c->k_stride, c->n_pages, c->page, vec), pool_units(c->v_stride, c->n_pages, c->page, vec)};
   if (last[0] < 0 || last[1] < 0) return fail(SM_ERR_SHAPE, "%s: a pool has strides of at least zero and spans at most 64 GiB", who);
-  if (!paged_attention_fits(c->n_req, c->heads_q, c->heads_kv, (int64_t)c->page * c->max_pages)) return fail(SM_ERR_SHAPE, "%s: too many requests and heads for one launch", who);
+  if (!paged_attention_fits(c->dtype, c->n_req, c->heads_q, c->heads_kv, c->d, (int64_t)c->page * c->max_pages)) return fail(SM_ERR_SHAPE, "%s: too many requests, heads and keys for one launch", who);
   return SM_OK;
 }
 }  // namespace
 
 extern "C" size_t sm_paged_attention_workspace_bytes(const sm_paged_attention_desc* c) {
   if (check_paged_attention(c, "sm_paged_attention_workspace_bytes") != SM_OK) return 0;
-  return paged_attention_workspace(c->dtype, c->n_req, c->heads_q, c->heads_kv, c->d, c->page, c->max_pages);
+  return paged_attention_workspace(c->dtype, c->n_req, c->heads_q, c->heads_kv, c->d, (int64_t)c->page * c->max_pages);
 }
 
 extern "C" int sm_paged_attention(const sm_paged_attention_desc* c, const void* q, const void* k_pages, const void* v_pages, const int32_t* table,
@@ -128,7 +128,7 @@ extern "C" int sm_paged_attention(const sm_paged_attention_desc* c, const void* 
   if (!q || !k_pages || !v_pages || !table || !lens || !o || !ws) return fail(SM_ERR_INVALID_ARG, "%s: null pointer", who);
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || !aligned16(ws)) return fail(SM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
   if (!aligned4(table) || !aligned4(lens) || !aligned4(lse)) return fail(SM_ERR_INVALID_ARG, "%s: table, lens and lse must be 4-byte aligned", who);
-  const size_t want = paged_attention_workspace(c->dtype, c->n_req, c->heads_q, c->heads_kv, c->d, c->page, c->max_pages);
+  const size_t want = paged_attention_workspace(c->dtype, c->n_req, c->heads_q, c->heads_kv, c->d, (int64_t)c->page * c->max_pages);
   if (ws_bytes < want) return fail(SM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, want);
   PagedAttnArgs a{q, k_pages, v_pages, table, lens, o, lse, (float*)ws, c->n_req, c->heads_q, c->heads_kv, c->d, c->page, c->max_pages, c->n_pages, c->scale,
                   c->table_pitch, c->q_stride[0], c->q_stride[1], c->o_stride[0], c->o_stride[1], c->k_stride[0], c->k_stride[1], c->k_stride[2],

@@ -35,8 +35,8 @@ struct PagedAttnArgs {
   float scale;
   int64_t pitch, q_r, q_h, o_r, o_h, k_page, k_t, k_h, v_page, v_t, v_h;
 };
-bool paged_attention_fits(int n_req, int heads_q, int heads_kv, int64_t max_keys);      // whether one launch can hold the call
-size_t paged_attention_workspace(int dtype, int n_req, int heads_q, int heads_kv, int d, int page, int max_pages);
+bool paged_attention_fits(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t max_keys);      // whether one launch can hold the call
+size_t paged_attention_workspace(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t max_keys);
 int launch_paged_attention(const PagedAttnArgs& a, int dtype, void* stream, int* launches);
 
 struct LinearW4Args {
