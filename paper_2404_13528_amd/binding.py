@@ -801,7 +801,7 @@ def _refuse(t, name, dtype, shape, device, rows):
 def _flat(t, name, dtype, shape, device):
     """The address of a contiguous device tensor of that type and shape."""
     try:
-        if t.dtype == dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
             return t.data_ptr()
     except AttributeError:
         pass
@@ -811,7 +811,7 @@ def _flat(t, name, dtype, shape, device):
 def _rows(t, name, dtype, shape, device):
     """The address of a device tensor of that type and shape whose last axis is contiguous."""
     try:
-        if t.dtype == dtype and t.shape == shape and t.device == device and (shape[-1] == 1 or t.stride(-1) == 1):
+        if t.dtype is dtype and t.shape == shape and t.device == device and (t.stride(-1) == 1 or shape[-1] == 1):
             return t.data_ptr()
     except AttributeError:
         pass
@@ -898,37 +898,48 @@ def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gam
     first = q if q is not None else k if k is not None else v
     if first is None:
         raise ValueError("q, k and v are all None")
-    T, heads, d = _dims(first, "q" if q is not None else "k" if k is not None else "v", 3)
+    T, heads, d = _dims(first, "q, k and v", 3)
     dt, dev, i32 = first.dtype, _device(), torch.int32
-    hq, hkv = (heads if q is not None else 0), (0 if k is None and v is None else _dims(k if k is not None else v, "k" if k is not None else "v", 3)[1])
-    pos = _flat(positions, "positions", i32, (T,), dev)
-    at, n_pages, page, kv_shape = None, 0, 0, (T, hkv, d)
+    qp = kp = vp = qo = ko = vo = at = None
+    hq = hkv = n_pages = page = 0
+    qs = qos = ks = vs = (0, 0)
+    kos = vos = (0, 0, 0)
+    if q is not None:
+        hq, shape = heads, (T, heads, d)
+        qp = _rows(q, "q", dt, shape, dev)
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=dt, device=dev)
+        qo = _rows(q_out, "q_out", dt, shape, dev)
+        qs, qos = q.stride()[:2], q_out.stride()[:2]
+    if k is not None or v is not None:
+        hkv = _dims(k if k is not None else v, "k and v", 3)[1]
+        shape = out_shape = (T, hkv, d)
+        if slots is not None:
+            n_pages, page, _, _ = _dims(k_out if k is not None else v_out, "the page pool of k / v", 4)
+            out_shape = (n_pages, page, hkv, d)
+        if k is not None:
+            kp = _rows(k, "k", dt, shape, dev)
+            if k_out is None:
+                k_out = torch.empty(shape, dtype=dt, device=dev)
+            ko = _rows(k_out, "k_out", dt, out_shape, dev)
+            ks, kos = k.stride()[:2], k_out.stride()[:-1]
+        if v is not None:
+            vp = _rows(v, "v", dt, shape, dev)
+            if v_out is None and slots is None:
+                v_out = torch.empty(shape, dtype=dt, device=dev)
+            vo = _rows(v_out, "v_out", dt, out_shape, dev)
+            vs, vos = v.stride()[:2], v_out.stride()[:-1]
+        if slots is None:                         # (row t of a pool of one page)
+            kos, vos = (0,) + kos[-2:], (0,) + vos[-2:]
     if slots is not None:
         at = _flat(slots, "slots", i32, (T,), dev)
-        if k is not None or v is not None:
-            n_pages, page = _dims(k_out if k is not None else v_out, "the page pool of k / v", 4)[:2]
-            kv_shape = (n_pages, page, hkv, d)
-    xs, ys, in_st, out_st, outs = [], [], [], [], []
-    for name, x, y, shape in (("q", q, q_out, (T, hq, d)), ("k", k, k_out, kv_shape), ("v", v, v_out, kv_shape)):
-        plain = name == "q" or slots is None
-        if x is None:
-            xs.append(None), ys.append(None), outs.append(None)
-            in_st += (0, 0)
-            out_st += (0, 0) if name == "q" else (0, 0, 0)
-            continue
-        xs.append(_rows(x, name, dt, (T, shape[-2], d), dev))
-        if y is None and plain:
-            y = torch.empty(shape, dtype=dt, device=dev)
-        ys.append(_rows(y, name + "_out", dt, shape, dev))
-        outs.append(y)
-        in_st += x.stride()[:2]
-        out_st += y.stride()[:-1] if name == "q" or not plain else (0,) + y.stride()[:2]
-    gains = [0 if g is None else _flat(g, name, dt, (d,), dev)
-             for name, g in (("q_gamma", q_gamma), ("q_beta", q_beta), ("k_gamma", k_gamma), ("k_beta", k_beta))]
-    desc = _HEAD_NORM_ROPE.pack(_dt(first), T, hq, hkv, d, HEAD_NORM[norm], eps, *gains, d if rot is None else int(rot), rope_base, page, n_pages,
-                                *in_st, *out_st)
-    check(lib().sm_head_norm_rope(desc, *xs, pos, at, *ys, _raw_stream(dev, stream)), "sm_head_norm_rope")
-    return tuple(outs)
+    vec = (d,)
+    desc = _HEAD_NORM_ROPE.pack(_dt(first), T, hq, hkv, d, HEAD_NORM[norm], eps, 0 if q_gamma is None else _flat(q_gamma, "q_gamma", dt, vec, dev),
+                                0 if q_beta is None else _flat(q_beta, "q_beta", dt, vec, dev), 0 if k_gamma is None else _flat(k_gamma, "k_gamma", dt, vec, dev),
+                                0 if k_beta is None else _flat(k_beta, "k_beta", dt, vec, dev), d if rot is None else rot, rope_base, page, n_pages,
+                                *qs, *ks, *vs, *qos, *kos, *vos)
+    check(lib().sm_head_norm_rope(desc, qp, kp, vp, _flat(positions, "positions", i32, (T,), dev), at, qo, ko, vo, _raw_stream(dev, stream)), "sm_head_norm_rope")
+    return (None if q is None else q_out), (None if k is None else k_out), (None if v is None else v_out)
 
 
 class PagedAttentionDesc(C.Structure):
