@@ -136,20 +136,37 @@ __device__ __forceinline__ PaWhere pa_where(const PagedAttnArgs& a, const PaUnit
   return w;
 }
 
+// A load of K takes 128 bytes of 8 keys, whole lines of memory (64 bytes of 16 keys, as the product wants them, would ask for every line
+// twice); two of them become two operands when lanes 8 .. 15 of a row of lanes change places with lanes 0 .. 7 of the other (pa_order_k).
 template <typename T, int DP, bool FULL>
 __device__ __forceinline__ void pa_load_k(PaTile<T, DP>& t, const unsigned where, const char* kb, const int d) {
   typedef PaTile<T, DP> Tile;
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4, piece = (c >> 3) * 4 + g;
   constexpr int SUB = Tile::TK / 16, STEPS = Tile::NK / SUB, E = 16 / (int)sizeof(T);
 #pragma unroll
   for (int j = 0; j < SUB; ++j) {
-    const char* p = kb + (uint64_t)__shfl(where, 16 * j + c, 64) * 16 + g * 16;
+    const char* pa = kb + (uint64_t)__shfl(where, 16 * j + (c & 7), 64) * 16 + piece * 16;
+    const char* pb = kb + (uint64_t)__shfl(where, 16 * j + (c & 7) + 8, 64) * 16 + piece * 16;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {
-      if (FULL || (s * 4 + g) * E < d) t.k[j * STEPS + s] = *(const pa_u32x4*)(p + s * 64);
-      else t.k[j * STEPS + s] = pa_u32x4{0, 0, 0, 0};
+    for (int s = 0; s < STEPS; s += 2) {
+      t.k[j * STEPS + s] = t.k[j * STEPS + s + 1] = pa_u32x4{0, 0, 0, 0};
+      if (FULL || (s * 4 + piece) * E < d) {
+        t.k[j * STEPS + s] = *(const pa_u32x4*)(pa + s * 64);
+        t.k[j * STEPS + s + 1] = *(const pa_u32x4*)(pb + s * 64);
+      }
     }
   }
+}
+template <typename T, int DP>
+__device__ __forceinline__ void pa_order_k(PaTile<T, DP>& t) {
+#pragma unroll
+  for (int i = 0; i < PaTile<T, DP>::NK; i += 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int a = t.k[i][e], b = t.k[i + 1][e];
+      t.k[i][e] = __builtin_amdgcn_update_dpp(a, b, 0x128, 0xf, 0xc, false);          // row_ror 8
+      t.k[i + 1][e] = __builtin_amdgcn_update_dpp(b, a, 0x128, 0xf, 0x3, false);
+    }
 }
 template <typename T, int DP, bool FULL>
 __device__ __forceinline__ void pa_load_v(PaTile<T, DP>& t, const unsigned where, const char* vb, const int d) {
@@ -319,6 +336,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 && PA_WAVES
       const unsigned mask = (unsigned)__ballot(at.on) & (TK == 32 ? 0xffffffffu : 0xffffu);
       float s[Tile::NV];
       __builtin_amdgcn_sched_barrier(0);
+      pa_order_k<T, DP>(t);
       pa_logits<T, DP>(t, [&](int i) { return Q_LDS ? s_q[i * 64 + lane] : q[Q_LDS ? 0 : i]; }, p.scale_log2e, s);
       key += STEP;
       at = pa_where(a, units, id, key, it.k1);
