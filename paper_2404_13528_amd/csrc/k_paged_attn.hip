@@ -82,34 +82,43 @@ __device__ __forceinline__ unsigned pa_chunks(int len, unsigned chunk) { return 
 __device__ __forceinline__ PaItem pa_item(const PaArgs& p, const unsigned item) {
   const int lane = threadIdx.x & 63, R = p.a.n_req, per = (R + 63) / 64;
   const int r0 = min(R, lane * per), r1 = min(R, r0 + per);
-  const int len0 = r0 < r1 ? pa_len(p.a, r0) : 0;      // (of a lane's first request; up to 64 requests need no other)
-  unsigned mine = (unsigned)(len0 + PA_UNIT - 1) / PA_UNIT;
-  for (int r = r0 + 1; r < r1; ++r) mine += (unsigned)(pa_len(p.a, r) + PA_UNIT - 1) / PA_UNIT;
+  constexpr int KEEP = 4;                              // lengths of a lane that stay in registers: all, up to 256 requests
+  int len[KEEP];
+  unsigned mine = 0;
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j) len[j] = pa_len(p.a, min(r0 + j, R - 1));      // (no branch: the loads go out together)
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j) len[j] = r0 + j < r1 ? len[j] : 0;
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j) mine += (unsigned)(len[j] + PA_UNIT - 1) / PA_UNIT;
+  for (int r = r0 + KEEP; r < r1; ++r) mine += (unsigned)(pa_len(p.a, r) + PA_UNIT - 1) / PA_UNIT;
   // (a lane's units fit 32 bits, their sum over the lanes is taken in two halves)
   const uint64_t units = (uint64_t)__builtin_amdgcn_readlane(pa_scan(mine & 0xffffu), 63) + ((uint64_t)__builtin_amdgcn_readlane(pa_scan(mine >> 16), 63) << 16);
   const uint64_t total = units * (unsigned)p.s.groups;
   const uint64_t share = (total + (1u << p.s.fill_log2) - 1) >> p.s.fill_log2, many = (total + (1u << PA_MANY_LOG2) - 1) >> PA_MANY_LOG2;
   const uint64_t want = share <= (uint64_t)p.s.cap ? share : max((uint64_t)p.s.cap, many);
   const unsigned chunk = max((unsigned)p.s.least, (unsigned)min(want, (uint64_t)1 << 23));
-  mine = r0 < r1 ? pa_chunks(len0, chunk) : 0;
-  for (int r = r0 + 1; r < r1; ++r) mine += pa_chunks(pa_len(p.a, r), chunk);
+  mine = 0;
+#pragma unroll
+  for (int j = 0; j < KEEP; ++j) mine += r0 + j < r1 ? pa_chunks(len[j], chunk) : 0;
+  for (int r = r0 + KEEP; r < r1; ++r) mine += pa_chunks(pa_len(p.a, r), chunk);
   const unsigned end = pa_scan(mine);
   PaItem it = {-1, 0, 0, 0};
   const uint64_t holds = __ballot(item < end);
   if (!holds) return it;
   const int src = __builtin_ctzll(holds);
   unsigned first = __builtin_amdgcn_readlane(end, src) - __builtin_amdgcn_readlane(mine, src);
-  int r = src * per, len = __builtin_amdgcn_readlane(len0, src);
-  for (;;) {                                           // (ends: the lane's requests have the item)
-    const unsigned n = pa_chunks(len, chunk);
-    if (item < first + n) {
-      const int64_t k0 = (int64_t)(item - first) * chunk * PA_UNIT;
-      it = {r, (int)k0, (int)min(k0 + (int64_t)chunk * PA_UNIT, (int64_t)len), (int)n};
-      break;
-    }
+  int r = src * per, l = 0;
+  unsigned n = 0;
+  for (int j = 0;; ++j) {                              // (ends: the lane's requests have the item)
+    l = j == 0 ? __builtin_amdgcn_readlane(len[0], src) : j == 1 ? __builtin_amdgcn_readlane(len[1], src) : j == 2 ? __builtin_amdgcn_readlane(len[2], src) :
+        j == 3 ? __builtin_amdgcn_readlane(len[3], src) : pa_len(p.a, r + j);
+    n = pa_chunks(l, chunk);
+    if (item < first + n) { r += j; break; }
     first += n;
-    len = pa_len(p.a, ++r);
   }
+  const int64_t k0 = (int64_t)(item - first) * chunk * PA_UNIT;
+  it = {r, (int)k0, (int)min(k0 + (int64_t)chunk * PA_UNIT, (int64_t)l), (int)n};
   it.r = __builtin_amdgcn_readfirstlane(it.r); it.k0 = __builtin_amdgcn_readfirstlane(it.k0);
   it.k1 = __builtin_amdgcn_readfirstlane(it.k1); it.n = __builtin_amdgcn_readfirstlane(it.n);
   return it;
@@ -290,7 +299,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 && PA_WAVES
   typedef PaTile<T, DP> Tile;
   constexpr int TK = Tile::TK, STEPS = Tile::NK / (TK / 16), E = 16 / (int)sizeof(T);
   constexpr bool Q_LDS = DP == 256;                 // the widest head's query operand takes its registers' place in LDS, under the results
-  __shared__ alignas(16) float s_o[PA_WAVES][PA_ROWS][DP];
+  __shared__ alignas(16) float s_o[PA_WAVES][PA_ROWS][DP + 4];      // (rows four banks apart)
   __shared__ float s_m[PA_WAVES][PA_ROWS], s_l[PA_WAVES][PA_ROWS];
   pa_u32x4* s_q = (pa_u32x4*)s_o;
   const PagedAttnArgs& a = p.a;
@@ -353,10 +362,12 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 && PA_WAVES
   l += __shfl_xor(l, 32, 64);
   if constexpr (Q_LDS) __syncthreads();
   if (g == 0) { s_m[w][c] = m; s_l[w][c] = l; }
+  if (c < rows) {
 #pragma unroll
-  for (int n = 0; n < Tile::EV; ++n)
+    for (int n = 0; n < Tile::EV; n += 4)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s_o[w][c][(4 * g + i) * Tile::EV + n] = o[n][i];
+      for (int i = 0; i < 4; ++i) *(pa_f32x4*)&s_o[w][c][(4 * g + i) * Tile::EV + n] = pa_f32x4{o[n][i], o[n + 1][i], o[n + 2][i], o[n + 3][i]};
+  }
   __syncthreads();
   float* part = a.part + ((int64_t)item * p.s.groups + grp) * pa_record(p.s.rows, a.d);
   if (grp == 0 && it.k0 == 0 && threadIdx.x == 0) p.plan[it.r] = make_int2(item, it.n);
