@@ -32,14 +32,14 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 pa_bf16x8;
 constexpr int PA_ROWS = 16;               // query heads a workgroup serves at once
 constexpr int PA_UNIT = 128;              // keys: chunks are whole units
 
-// How the work is cut.  A chunk's start costs some 5 us (lengths, page table, first keys: three trips to memory), so a chunk is as long as
-// lets all workgroups be resident at once; but where that makes it longer than 512 KB of keys and values, up to 4096 shorter ones balance
-// the load better than they cost (64 requests of 100 to 30000 keys: 272 us instead of 288; one request of 131071 keys is best off
-// with the 1024 that fit).
+// How the work is cut.  A chunk's start costs some 4 us (lengths, page table, first keys: three trips to memory), so at first there are as
+// many chunks as two workgroups a CU (heads over 128: one): 64 requests of 1000 keys take 54 us, with twice as many chunks 62.  But where
+// that makes a chunk longer than 512 KB of keys and values, up to 4096 shorter ones balance the load better than they cost (64 requests of
+// 100 to 30000 keys: 271 us instead of 288).
 constexpr int PA_MANY_LOG2 = 12;
 struct PaShape {
   int rows, tiles, groups;                // query heads per tile, tiles per key head, workgroups per chunk
-  int fill_log2, cap, least;              // workgroups that fit, units of a long and of the shortest chunk
+  int fill_log2, cap, least;              // workgroups at first, units of a long and of the shortest chunk
   int items;                              // chunks at most
 };
 PaShape pa_shape(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t max_keys) {
@@ -48,7 +48,7 @@ PaShape pa_shape(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t
   s.rows = std::min(g, PA_ROWS);
   s.tiles = (g + PA_ROWS - 1) / PA_ROWS;
   s.groups = heads_kv * s.tiles;
-  s.fill_log2 = d > 128 ? 9 : 10;
+  s.fill_log2 = d > 128 ? 8 : 9;
   s.cap = std::max(1, (512 << 10) / (2 * d * (dtype == 0 ? 4 : 2) * PA_UNIT));
   s.least = max_keys <= 2 * PA_UNIT ? 2 : 1;          // (256 keys are one workgroup's, without a join)
   const int64_t units = (max_keys + PA_UNIT - 1) / PA_UNIT, share = (n_req * units * s.groups + (1 << s.fill_log2) - 1) >> s.fill_log2;
@@ -74,7 +74,7 @@ __device__ __forceinline__ unsigned pa_scan(unsigned x) {
 }
 
 // The chunk of workgroup `item`: request (-1: none), first key, one behind the last key, number of the request's chunks.
-// A lane has `per` requests.  With U units in all, `share` = U groups / 2^fill units would fill the chip; every request has at least one
+// A lane has `per` requests.  With U units in all, `share` = U groups / 2^fill units would make 2^fill workgroups; every request has at least one
 // chunk, so chunks of at least that length are at most 2^fill / groups + n_req.
 struct PaItem { int r, k0, k1, n; };
 __device__ __forceinline__ int pa_len(const PagedAttnArgs& a, int r) { return min(max(a.lens[r], 0), a.max_pages * a.page); }

@@ -77,7 +77,7 @@ def test_page_table_small(cached, fresh, page, cols):
         page_case(cached, fresh, page, cols, pad=pad, short=short, pitch=pitch)
 
 
-@pytest.mark.parametrize("R", [1, 63, 64, 65, 255, 256, 257, 511, 1000, 2049])
+@pytest.mark.parametrize("R", [1, 63, 64, 65, 255, 256, 257, 511, 768, 769, 1000, 1024, 1025, 2049, 5000])
 def test_page_table_many_requests(R):
     rng = np.random.default_rng(R)
     cached = rng.integers(0, 50, R).tolist()
@@ -98,6 +98,19 @@ def test_page_table_without_tokens_or_free_pages():
 def test_page_table_bad_pages_have_no_slot():
     out = sm.page_table(ints([1, 1, 0]), ints([1, 1, 2]), ints([99, 2]), ints([2]), ints([[-3], [64], [5]]), 16, 64, 4)
     assert out.slots.tolist() == [-1, -1, -1, -1] and out.lens.tolist() == [2, 2, 2]
+
+
+def test_page_table_counts_at_the_limits():
+    """Lengths and capacities at 2^30, where sums of two of them do not fit 31 bits."""
+    big = 2 ** 30
+    i = 2 ** 31 - 1
+    out = sm.page_table(ints([i, 5]), ints([i, i]), ints([0]), ints([1]), ints([[0], [0]]), big, 1, 300)
+    # the first request's row is full; all 300 rows are its tokens, without a slot; the second keeps its five
+    assert out.starts.tolist() == [0, 300, 300] and out.lens.tolist() == [big, 5] and out.need.item() == 0
+    assert (out.slots == -1).all() and out.positions[:2].tolist() == [big, big + 1] and out.positions[299].item() == big + 299
+    out = sm.page_table(ints([0, big - 2]), ints([3, i]), ints([]), ints([i]), ints([[0], [0]]), big, 1, 8)
+    assert out.starts.tolist() == [0, 3, 8] and out.lens.tolist() == [0, big] and out.need.item() == 1
+    assert out.slots.tolist() == [-1, -1, -1, big - 2, big - 1, -1, -1, -1]
 
 
 # ------------------------------------------------------------------------------------------------ norm + rotation + store
