@@ -408,16 +408,17 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
   const float* base = a.part + ((int64_t)pl.x * p.s.groups + hk * p.s.tiles + qt) * pa_record(p.s.rows, a.d);
   float m = -INFINITY, l = 0.f;
   pa_f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  constexpr int U = 8;
+  constexpr int U = 4;
   for (int i0 = grp; i0 < pl.y; i0 += ng * U) {
     float mi[U], li[U];
     pa_f32x4 oi[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      // (no branch around a load: the loads go out together; the last chunk again where there is none)
       const float* q = base + (int64_t)min(i0 + u * ng, pl.y - 1) * rec;
       const float2 ml = *(const float2*)(q + p.s.rows * a.d + 2 * row);
       mi[u] = i0 + u * ng < pl.y ? ml.x : -INFINITY; li[u] = ml.y;
-      oi[u] = e < d4 ? *(const pa_f32x4*)(q + row * a.d + 4 * e) : pa_f32x4{0.f, 0.f, 0.f, 0.f};
+      oi[u] = *(const pa_f32x4*)(q + row * a.d + 4 * min(e, d4 - 1));
     }
     float mn = m;
 #pragma unroll
