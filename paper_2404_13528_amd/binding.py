@@ -854,6 +854,7 @@ class PageCfg(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_req", "page", "max_pages", "n_pages", "free_cap", "max_tokens")] + [("table_pitch", C.c_int64)]
 
 
+_PAGE_CFG = struct.Struct("@6iq")
 PageTable = collections.namedtuple("PageTable", "starts lens positions slots need")
 
 
@@ -865,16 +866,21 @@ def page_table(cached, fresh, free_pages, n_free, table, page, n_pages, max_toke
     i32, dev = torch.int32, _device()
     R, cols = _dims(table, "table", 2)
     free_cap, = _dims(free_pages, "free_pages", 1)
-    n = max(0, int(max_tokens))
-    cfg = PageCfg(R, int(page), cols, int(n_pages), free_cap, int(max_tokens), table.stride(0) if R > 1 else cols)
-    ins = (_flat(cached, "cached", i32, (R,), dev), _flat(fresh, "fresh", i32, (R,), dev), _flat(free_pages, "free_pages", i32, (free_cap,), dev),
+    n, one = max(0, max_tokens), (R,)
+    ins = (_flat(cached, "cached", i32, one, dev), _flat(fresh, "fresh", i32, one, dev), _flat(free_pages, "free_pages", i32, (free_cap,), dev),
            _flat(n_free, "n_free", i32, (1,), dev), _rows(table, "table", i32, (R, cols), dev))
+    cfg = _PAGE_CFG.pack(R, page, cols, n_pages, free_cap, max_tokens, table.stride(0) if R > 1 else cols)
     sizes = (R + 1, R, n, n, 1)
     if out is None:
-        out = PageTable(*torch.empty(sum(sizes), dtype=i32, device=dev).split(sizes))
-    ptrs = [_flat(t, name, i32, (k,), dev) for t, name, k in zip(out, PageTable._fields, sizes)]
-    check(lib().sm_page_table(C.byref(cfg), *ins, *ptrs, _raw_stream(dev, stream)), "sm_page_table")
-    return out
+        whole = torch.empty(2 * (R + n + 1), dtype=i32, device=dev)
+        at = whole.data_ptr()
+        lens = at + 4 * (R + 1)
+        pos = lens + 4 * R
+        ptrs = (at, lens, pos, pos + 4 * n, pos + 8 * n)
+    else:
+        ptrs = [_flat(t, name, i32, (k,), dev) for t, name, k in zip(out, PageTable._fields, sizes)]
+    check(lib().sm_page_table(cfg, *ins, *ptrs, _raw_stream(dev, stream)), "sm_page_table")
+    return PageTable(*whole.split(sizes)) if out is None else out
 
 
 class HeadNormRopeDesc(C.Structure):
@@ -909,7 +915,9 @@ def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gam
         qp = _rows(q, "q", dt, shape, dev)
         if q_out is None:
             q_out = torch.empty(shape, dtype=dt, device=dev)
-        qo = _rows(q_out, "q_out", dt, shape, dev)
+            qo = q_out.data_ptr()
+        else:
+            qo = _rows(q_out, "q_out", dt, shape, dev)
         qs, qos = q.stride()[:2], q_out.stride()[:2]
     if k is not None or v is not None:
         hkv = _dims(k if k is not None else v, "k and v", 3)[1]
@@ -973,8 +981,11 @@ class PagedAttention:
         c, dt, dev, i32 = self.desc, self.dtype, _device(), torch.int32
         if out is None:
             out = torch.empty(self.q_shape, dtype=dt, device=dev)
+            op = out.data_ptr()
+        else:
+            op = _rows(out, "out", dt, self.q_shape, dev)
         args = (_rows(q, "q", dt, self.q_shape, dev), _rows(k_pages, "k_pages", dt, self.pool_shape, dev), _rows(v_pages, "v_pages", dt, self.pool_shape, dev),
-                _rows(table, "table", i32, self.table_shape, dev), _flat(lens, "lens", i32, self.q_shape[:1], dev), _rows(out, "out", dt, self.q_shape, dev),
+                _rows(table, "table", i32, self.table_shape, dev), _flat(lens, "lens", i32, self.q_shape[:1], dev), op,
                 None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(self.ws, "the workspace", torch.uint8, self.ws.shape, dev))
         c.table_pitch = table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1]
         c.q_stride[:], c.o_stride[:] = q.stride()[:2], out.stride()[:2]
@@ -986,6 +997,8 @@ class PagedAttention:
 class LinearW4Desc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("M", "N", "K", "group", "act")]
 
+
+_LINEAR_W4 = struct.Struct("@5i")
 
 class LinearW4:
     """sm_linear_w4: a Linear whose weights stay in 4 bits.  w [N, K / 2] uint8 (even k in the low four bits), scales [N, K / group]
@@ -1015,10 +1028,12 @@ class LinearW4:
         xp, shape = _flat(x, "x", bf16, (M, self.K), dev), (M, self.N)
         if out is None:
             out = torch.empty(shape, dtype=bf16, device=dev)
-        d = LinearW4Desc(M, self.N, self.K, self.group, ACT[act])
-        check(lib().sm_linear_w4(C.byref(d), xp, _flat(self.packed, "the packed weights", torch.uint8, self.packed.shape, dev),
+            op = out.data_ptr()
+        else:
+            op = _flat(out, "out", bf16, shape, dev)
+        check(lib().sm_linear_w4(_LINEAR_W4.pack(M, self.N, self.K, self.group, ACT[act]), xp, _flat(self.packed, "the packed weights", torch.uint8, self.packed.shape, dev),
                                  None if self.bias is None else self.bias.data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev),
-                                 _flat(out, "out", bf16, shape, dev), _raw_stream(dev, stream)), "sm_linear_w4")
+                                 op, _raw_stream(dev, stream)), "sm_linear_w4")
         return out
 
 

@@ -38,8 +38,8 @@ extern "C" int sm_page_table(const sm_page_cfg* c, const int32_t* cached, const 
   for (const void* p : all) if (!aligned4(p)) return fail(SM_ERR_INVALID_ARG, "%s: arrays must be 4-byte aligned", who);
   PageTableArgs a{cached, fresh, free_pages, n_free, table, starts, lens, positions, slots, need,
                   c->n_req, c->page, c->max_pages, c->n_pages, c->free_cap, c->max_tokens, c->table_pitch};
-  char label[96];
-  snprintf(label, sizeof(label), "page_table[%d,%d]", c->n_req, c->max_tokens);
+  char label[96] = "";
+  if (timing_on()) snprintf(label, sizeof(label), "page_table[%d,%d]", c->n_req, c->max_tokens);
   Timed tm(label, stream);
   if (int e = launch_page_table(a, stream)) return fail(SM_ERR_DEVICE, "%s: launch failed (hip error %d)", who, e);
   count_compute();
@@ -86,8 +86,8 @@ extern "C" int sm_head_norm_rope(const sm_head_norm_rope_desc* c, const void* q,
   }
   a.positions = positions; a.slots = slots; a.tokens = c->tokens; a.d = c->d; a.rot = c->rot; a.norm = c->norm;
   a.page = slots ? c->page : 1; a.n_slots = slots ? c->page * c->n_pages : 0; a.eps = c->eps;
-  char label[128];
-  snprintf(label, sizeof(label), "head_norm_rope_%s[%d,%d+%d+%d,%d]%s", c->dtype == SM_F32 ? "f32" : "bf16", c->tokens, q ? c->heads_q : 0, k ? c->heads_kv : 0,
+  char label[128] = "";
+  if (timing_on()) snprintf(label, sizeof(label), "head_norm_rope_%s[%d,%d+%d+%d,%d]%s", c->dtype == SM_F32 ? "f32" : "bf16", c->tokens, q ? c->heads_q : 0, k ? c->heads_kv : 0,
            v ? c->heads_kv : 0, c->d, slots ? "+pages" : "");
   Timed tm(label, stream);
   if (int e = launch_head_norm_rope(a, c->dtype, stream)) return fail(SM_ERR_DEVICE, "%s: launch failed (hip error %d)", who, e);
@@ -133,8 +133,8 @@ extern "C" int sm_paged_attention(const sm_paged_attention_desc* c, const void* 
   PagedAttnArgs a{q, k_pages, v_pages, table, lens, o, lse, (float*)ws, c->n_req, c->heads_q, c->heads_kv, c->d, c->page, c->max_pages, c->n_pages, c->scale,
                   c->table_pitch, c->q_stride[0], c->q_stride[1], c->o_stride[0], c->o_stride[1], c->k_stride[0], c->k_stride[1], c->k_stride[2],
                   c->v_stride[0], c->v_stride[1], c->v_stride[2]};
-  char label[128];
-  snprintf(label, sizeof(label), "paged_attention_%s[%d,%d/%d,%d,%d]", c->dtype == SM_F32 ? "f32" : "bf16", c->n_req, c->heads_q, c->heads_kv, c->max_pages * c->page, c->d);
+  char label[128] = "";
+  if (timing_on()) snprintf(label, sizeof(label), "paged_attention_%s[%d,%d/%d,%d,%d]", c->dtype == SM_F32 ? "f32" : "bf16", c->n_req, c->heads_q, c->heads_kv, c->max_pages * c->page, c->d);
   Timed tm(label, stream);
   int launches = 0;
   if (int e = launch_paged_attention(a, c->dtype, stream, &launches)) return fail(SM_ERR_DEVICE, "%s: launch failed (hip error %d)", who, e);
@@ -175,8 +175,8 @@ extern "C" int sm_linear_w4(const sm_linear_w4_desc* c, const void* x, const voi
   if (!x || !packed || !y) return fail(SM_ERR_INVALID_ARG, "%s: null pointer", who);
   if (!aligned16(x) || !aligned16(packed) || !aligned16(y) || !aligned16(bias) || !aligned16(residual)) return fail(SM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
   LinearW4Args a{x, packed, bias, residual, y, c->M, c->N, c->K, c->group, c->act};
-  char label[96];
-  snprintf(label, sizeof(label), "linear_w4g%d[%d,%d,%d]%s%s", c->group, c->M, c->N, c->K, c->act ? "+gelu" : "", residual ? "+res" : "");
+  char label[96] = "";
+  if (timing_on()) snprintf(label, sizeof(label), "linear_w4g%d[%d,%d,%d]%s%s", c->group, c->M, c->N, c->K, c->act ? "+gelu" : "", residual ? "+res" : "");
   Timed tm(label, stream);
   if (int e = launch_w4(a, stream)) return fail(SM_ERR_DEVICE, "%s: launch failed (hip error %d)", who, e);
   count_compute();
