@@ -476,7 +476,7 @@ int sm_page_table(const sm_page_cfg*, const int32_t* cached, const int32_t* fres
  * A token with a negative position is padding: nothing is stored for it.  Two tokens of one slot: each head of
  * the slot holds either of them.  An output may be its input (same address and strides), otherwise they must not overlap.
  * Angles are exact to a 2^-31 revolution at any position.  rot a multiple of twice the 16-byte vector (16 bf16, 8 f32),
- * d a multiple of the vector, both at most 256; rope_base >= 1; n_pages * page <= 2^30. */
+ * d a multiple of the vector, both at most 256; rope_base >= 1; n_pages * page <= 2^30, tokens <= 2^25. */
 typedef struct {
   int32_t dtype, tokens, heads_q, heads_kv, d;
   int32_t norm; float eps;
@@ -493,7 +493,7 @@ int sm_head_norm_rope(const sm_head_norm_rope_desc*, const void* q, const void* 
  * multiple of heads_kv).  No token (lens[r] <= 0, or no page of them exists): o = 0, lse = -inf.  lse (nullable)
  * [n_req, heads_q] fp32, contiguous: the natural logarithm of the sum of exp(scale * q . k), with which results over
  * disjoint parts of a cache can be joined.  What lies in a page behind the request's last token is not used, whatever
- * it is.  Strides: request, head (q, o); page, token, head (k_pages, v_pages: token-major [page, token, head, d] and
+ * it is.  o must not overlap the inputs.  Strides: request, head (q, o); page, token, head (k_pages, v_pages: token-major [page, token, head, d] and
  * head-major [page, head, token, d] pools alike; page and token strides not negative, a pool's pages within 64 GiB).  The
  * key axis is split over workgroups by the lengths found on the device and joined in fp32.
  * d a multiple of the 16-byte vector (8 bf16, 4 f32), at most 256.  The workspace holds partial results; nothing in it
@@ -513,7 +513,8 @@ int sm_paged_attention(const sm_paged_attention_desc*, const void* q, const void
  * SM_ACT_NONE or SM_ACT_GELU (erf).  sm_linear_w4_pack writes weights, scales and zero points into `packed`
  * (sm_linear_w4_packed_bytes, caller-owned device memory) in the order the kernel reads them, once.  The products are
  * exact (integers times bf16, fp32 sums); a group's sum takes its scale in fp32; a row of x with an infinity or a NaN gives
- * NaN.  Made for the rows of a decode step: the weights are streamed once per 32 rows. */
+ * NaN.  y may be the residual, but must not overlap x.  Made for the rows of a decode step: the weights are streamed once
+ * per 32 rows at best. */
 typedef struct { int32_t M, N, K, group, act; } sm_linear_w4_desc;
 size_t sm_linear_w4_packed_bytes(int N, int K, int group);
 int sm_linear_w4_pack(const void* w, const void* scales, const void* zeros, int N, int K, int group, void* packed, void* stream);

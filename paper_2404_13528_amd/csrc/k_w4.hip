@@ -122,14 +122,15 @@ __device__ __forceinline__ void w4_store(const LinearW4Args& a, int row, int n, 
 // waves' sums of a tile meet in LDS.
 // Loads return in the order of their issue, and the compiler's counting of them survives no branch: all loads are unconditional, and their
 // order is pinned.
-// On the GPU, weights cold: 1 x 4096 x 4096 (groups of 128) 4.2 us, 1 x 22016 x 4096 12.8 us (3.7 TB/s), 32 x 22016 x 4096 18.5 us,
-// 32 x 4096 x 11008 22.8 us (704 KB of x for every workgroup).
+// On the GPU, weights cold: 1 x 4096 x 4096 (groups of 128) 4.2 us, 1 x 22016 x 4096 12.9 us (3.7 TB/s), 32 x 22016 x 4096 18.4 us,
+// 32 x 4096 x 11008 14.9 us.
 template <int MT, bool HALF, int NT, int GPB, int PB>
 __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
   constexpr int RT = NT * MT * W4_WAVES <= 96 ? NT : 96 / MT / W4_WAVES;       // tiles that meet at once
   __shared__ float red[W4_WAVES][RT][MT][16][17];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * 16 * MT, rows = min(16 * MT, p.a.M - m0), K = p.a.K;
+  constexpr int ROWS = HALF ? 8 : 16 * MT;
+  const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * ROWS, rows = min(ROWS, p.a.M - m0), K = p.a.K;
   const unsigned mask = p.mask;
   unsigned offset;
   asm("v_mov_b32 %0, %1" : "=v"(offset) : "s"(p.offset));      // (an instruction takes one scalar register: the other constant goes to a vector one)
@@ -237,27 +238,45 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
   }
 }
 
+// Rows and tiles of a workgroup.  The time goes by the bytes that a CU takes in: a workgroup's rows of x (2 a k) and tiles of weights (8 and a
+// half a k, scales included), times the workgroups that a CU has; a tile's sums that meet at the end count like 6 more.  Measured against all
+// 15 choices at eleven sizes the one taken was within 0.4 us of the best: 32 x 4096 x 4096 takes 7.1 us with 16 rows and two tiles, 10.3 with
+// 32 and one; 32 x 11008 x 4096 12.9 us with 32 and three, 25 with 16 and one; 1 x 22016 x 4096 12.5 to 13.9 us.
+struct W4Choice { int rows, nt; };
+static W4Choice w4_choose(int M, int tiles) {
+  static const int NTS[5] = {1, 2, 3, 4, 6};
+  W4Choice best = {0, 0};
+  double least = 0;
+  for (int rows = 8; rows <= 32; rows *= 2) {
+    if (rows > 8 && rows / 2 >= M) break;
+    if ((M + rows - 1) / rows > 65535) continue;       // (a launch's second extent)
+    for (int nt : NTS) {
+      const int64_t groups = (int64_t)((tiles + nt - 1) / nt) * ((M + rows - 1) / rows);
+      const double cost = (double)((groups + 255) / 256) * (2.0 * std::min(rows, M) + 8.5 * nt) + 6.0 * nt;
+      if (!best.rows || cost <= least) { best = W4Choice{rows, nt}; least = cost; }
+    }
+  }
+  return best;
+}
 template <int GPB, int MT, bool HALF, int NT>
 static void w4_go(const W4Args& p, hipStream_t stream) {
-  constexpr int PB = MT == 1 ? 2 : 1;
-  w4_kernel<MT, HALF, NT, GPB, PB><<<dim3((p.tiles + NT - 1) / NT, (p.a.M + 16 * MT - 1) / (16 * MT)), dim3(64 * W4_WAVES), 0, stream>>>(p);
+  constexpr int PB = MT == 1 ? 2 : 1, ROWS = HALF ? 8 : 16 * MT;
+  w4_kernel<MT, HALF, NT, GPB, PB><<<dim3((p.tiles + NT - 1) / NT, (p.a.M + ROWS - 1) / ROWS), dim3(64 * W4_WAVES), 0, stream>>>(p);
 }
-// Tiles per workgroup, 256 CUs: as many as make the launch one round of workgroups, since every one loads all of x.  Up to 16 rows that is
-// little and three tiles are enough (1 x 22016 x 4096: 12.8 us with 3, 13.5 with 6); beyond, six (32 rows: 18.5 us with 6, 22.1 with 3).
 template <int GPB, int MT, bool HALF>
-static void w4_tiles(const W4Args& p, hipStream_t stream) {
-  const int per_cu = (p.tiles + 255) / 256;
-  if (per_cu <= 1) w4_go<GPB, MT, HALF, 1>(p, stream);
-  else if (per_cu == 2) w4_go<GPB, MT, HALF, 2>(p, stream);
-  else if (per_cu == 3 || MT == 1) w4_go<GPB, MT, HALF, 3>(p, stream);
-  else if (per_cu == 4) w4_go<GPB, MT, HALF, MT == 1 ? 3 : 4>(p, stream);
-  else w4_go<GPB, MT, HALF, MT == 1 ? 3 : 6>(p, stream);
+static void w4_tiles(const W4Args& p, int nt, hipStream_t stream) {
+  if (nt == 1) w4_go<GPB, MT, HALF, 1>(p, stream);
+  else if (nt == 2) w4_go<GPB, MT, HALF, 2>(p, stream);
+  else if (nt == 3) w4_go<GPB, MT, HALF, 3>(p, stream);
+  else if (nt == 4) w4_go<GPB, MT, HALF, 4>(p, stream);
+  else w4_go<GPB, MT, HALF, 6>(p, stream);
 }
 template <int GPB>
 static void w4_launch(const W4Args& p, hipStream_t stream) {
-  if (p.a.M <= 8) w4_tiles<GPB, 1, true>(p, stream);
-  else if (p.a.M <= 16) w4_tiles<GPB, 1, false>(p, stream);
-  else w4_tiles<GPB, 2, false>(p, stream);
+  const W4Choice c = w4_choose(p.a.M, p.tiles);
+  if (c.rows == 8) w4_tiles<GPB, 1, true>(p, c.nt, stream);
+  else if (c.rows == 16) w4_tiles<GPB, 1, false>(p, c.nt, stream);
+  else w4_tiles<GPB, 2, false>(p, c.nt, stream);
 }
 int launch_w4(const LinearW4Args& a, void* stream) {
   const W4Args p{a, (a.K + W4_BLOCK - 1) / W4_BLOCK, (a.N + 15) / 16, 0x000f000fu, 0x43004300u};

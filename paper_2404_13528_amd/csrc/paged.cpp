@@ -52,7 +52,7 @@ extern "C" int sm_head_norm_rope(const sm_head_norm_rope_desc* c, const void* q,
   if (!c) return fail(SM_ERR_INVALID_ARG, "%s: null descriptor", who);
   if (!dtype_ok(c->dtype)) return fail(SM_ERR_INVALID_ARG, "%s: unknown dtype", who);
   const int vec = c->dtype == SM_F32 ? 4 : 8;
-  if (c->tokens < 0 || c->tokens > CAP) return fail(SM_ERR_SHAPE, "%s: bad number of tokens", who);
+  if (c->tokens < 0 || c->tokens > (1 << 25)) return fail(SM_ERR_SHAPE, "%s: 0 to 2^25 tokens", who);      // (a launch has less than 2^32 threads)
   if ((q && (c->heads_q < 1 || c->heads_q > 65536)) || ((k || v) && (c->heads_kv < 1 || c->heads_kv > 65536))) return fail(SM_ERR_SHAPE, "%s: bad number of heads", who);
   if (c->d < vec || c->d > 256 || c->d % vec) return fail(SM_ERR_SHAPE, "%s: head size must be a multiple of %d, at most 256", who, vec);
   if (c->rot < 0 || c->rot > c->d || c->rot % (2 * vec)) return fail(SM_ERR_SHAPE, "%s: rotated features must be a multiple of %d, at most the head size", who, 2 * vec);

@@ -51,6 +51,22 @@ def test_exact_sums(M, N, steps, group):
     case(M, N, steps * group, group, False, False, False, "none", seed=M + N + 1, exact=True)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N", [(1, 20503), (3, 8219), (3, 24610), (8, 48005), (9, 2077), (9, 4112), (16, 8219), (9, 12289), (13, 16396), (17, 2743), (31, 4112), (17, 8219),
+                                 (29, 12289), (17, 16396), (70, 4100)])
+def test_exact_sums_of_many_features(M, N, group):
+    """Enough features for every number of tiles that a workgroup may have, at 8, 16 and 32 rows."""
+    case(M, N, 3 * group, group, True, True, True, "none", seed=M + N, exact=True)
+
+
+def test_residual_may_be_the_result():
+    g = torch.Generator().manual_seed(8)
+    lin = sm.LinearW4(torch.randint(0, 256, (200, 64), generator=g, dtype=torch.uint8).cuda(), torch.rand(200, 2, generator=g).to(BF16).cuda(), group=64)
+    x, y = torch.randn(20, 128, generator=g).to(BF16).cuda(), torch.randn(20, 200, generator=g).to(BF16).cuda()
+    want = lin(x, residual=y)
+    assert torch.equal(lin(x, residual=y, out=y), want)
+
+
 @pytest.mark.parametrize("M,N,K,group,zeros,bias,residual,act", [
     (1, 4096, 4096, 128, True, False, False, "none"), (5, 1000, 2048, 64, False, True, False, "gelu"), (32, 515, 1024, 32, True, True, True, "gelu"),
     (8, 2048, 8192, 128, True, True, True, "none"), (1, 8, 16384, 32, False, False, True, "none"), (40, 300, 1152, 128, True, False, False, "gelu"),

@@ -53,7 +53,7 @@ def rope_call(d, q=A, k=A, v=A, positions=A, slots=A, q_out=A, k_out=A, v_out=A)
 
 
 @pytest.mark.parametrize("change,code", [
-    (dict(dtype=2), -1), (dict(tokens=-1), -2), (dict(heads_q=0), -2), (dict(heads_kv=0), -2), (dict(d=60), -2), (dict(d=264), -2), (dict(d=0), -2),
+    (dict(dtype=2), -1), (dict(tokens=-1), -2), (dict(tokens=(1 << 25) + 1), -2), (dict(heads_q=0), -2), (dict(heads_kv=0), -2), (dict(d=60), -2), (dict(d=264), -2), (dict(d=0), -2),
     (dict(rot=24), -2), (dict(rot=80), -2), (dict(rot=-16), -2), (dict(norm=3), -1), (dict(rope_base=0.5), -1), (dict(rope_base=float("nan")), -1),
     (dict(page=0), -2), (dict(n_pages=0), -2), (dict(n_pages=(1 << 26) + 1), -2), (dict(q_gamma=None), -1), (dict(k_gamma=None), -1),
     (dict(norm=1, q_beta=None), -1), (dict(norm=1, k_beta=None), -1), (dict(q_gamma=A.value + 8), -1), (dict(q_stride=(4, 64)), -2),
