@@ -189,6 +189,29 @@ def test_head_norm_rope_plain_rows_and_far_positions(dtype):
     head_norm_case(1500, 2, 1, 128, 128, "rms", dtype, page=8)
 
 
+@pytest.mark.parametrize("T", [767, 768, 900])
+def test_head_norm_rope_around_the_change_of_form(T):
+    """A token for four waves, or for one: the same results, in place and with parts left out as well."""
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn(T, 7, 96, generator=g).to(BF16).cuda()
+    gq, gk = (1 + 0.1 * torch.randn(2, 96, generator=g)).to(BF16).cuda()
+    pos = torch.randint(0, 9999, (T,), generator=g).to(I32).cuda()
+    pos[5] = -3
+    kw = dict(q_gamma=gq, k_gamma=gk, rot=32)
+    fill = [torch.zeros(T, n, 96, dtype=BF16, device="cuda") for n in (4, 1, 1)]
+    q, k, v = sm.head_norm_rope(x[:, :4], x[:, 4:5], x[:, 5:6], pos, q_out=fill[0], k_out=fill[1], v_out=fill[2], **kw)
+    for part in (slice(0, 300), slice(300, T)):                      # the few-token form, in two pieces
+        f = [torch.zeros(pos[part].shape[0], n, 96, dtype=BF16, device="cuda") for n in (4, 1, 1)]
+        got = sm.head_norm_rope(x[part, :4], x[part, 4:5], x[part, 5:6], pos[part], q_out=f[0], k_out=f[1], v_out=f[2], **kw)
+        assert all(torch.equal(a, b[part]) for a, b in zip(got, (q, k, v)))
+    k2 = sm.head_norm_rope(None, x[:, 4:5], None, pos, k_out=torch.zeros_like(k), **kw)[1]
+    assert torch.equal(k2, k)
+    y = x.clone()
+    sm.head_norm_rope(y[:, :4], y[:, 4:5], y[:, 5:6], pos, q_out=y[:, :4], k_out=y[:, 4:5], v_out=y[:, 5:6], **kw)
+    live = pos >= 0
+    assert torch.equal(y[live][:, :4], q[live]) and torch.equal(y[live][:, 4:5], k[live]) and torch.equal(y[~live], x[~live]) and torch.equal(y[:, 6], x[:, 6])
+
+
 def test_head_norm_rope_parts_in_place_and_empty():
     x = torch.randn(6, 4, 64, device="cuda")
     g = torch.ones(64, device="cuda")
@@ -315,6 +338,73 @@ def test_paged_attention_infinite_and_nan_keys_stay_in_their_request(dtype):
     vp[45, 3] = float("inf")
     got = att(q, kp, vp, table, lens)
     assert torch.equal(got[0], want[0]) and got[1].isnan().all() and (got[2] == float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("R", [64, 65, 256, 257, 1500])
+def test_paged_attention_many_requests(R, dtype):
+    """Several requests per lane of the scan that cuts the work, empty ones among them."""
+    rng = np.random.default_rng(R)
+    lens = (rng.integers(0, 400, R) * (rng.random(R) < 0.7)).tolist()
+    lens[R // 2], lens[-1] = 3000, 1
+    attn_case(lens, 2, 1, 32, 16, dtype, seed=R)
+
+
+def test_paged_attention_pools_of_different_layouts():
+    """Keys head-major, values token-major with a gap between heads, one page as long as the whole request."""
+    g = torch.Generator().manual_seed(12)
+    for dtype, page, n in ((BF16, 16, 200), (F32, 700, 650)):
+        cols = -(-n // page)
+        ids = torch.randperm(cols + 2, generator=g)[:cols].tolist()
+        kp = torch.randn(cols + 2, 3, page, 64, generator=g).to(dtype)
+        vp = torch.randn(cols + 2, page, 3, 2, 64, generator=g).to(dtype)
+        q = torch.randn(1, 6, 64, generator=g).to(dtype)
+        o, _, av, aw = P.paged_attention(to_np(q), to_np(kp.transpose(1, 2)), to_np(vp[:, :, :, 1]), np.array([ids]), [n], 0.125, want_bound=True)
+        got = sm.PagedAttention(1, 6, 3, 64, page, cols, cols + 2, dtype)(q.cuda(), kp.cuda().transpose(1, 2), vp.cuda()[:, :, :, 1], ints([ids]), ints([n]))
+        check(got, o, HALF[dtype] * np.abs(o) + (2 * (68 * 2.0 ** -24 * aw + 2.0 ** -20) + 2.0 ** -16) * av, "o")
+
+
+def test_paged_attention_captured_with_short_and_replayed_with_long_requests():
+    g = torch.Generator().manual_seed(13)
+    kp, vp = torch.randn(2, 300, 16, 2, 64, generator=g).to(BF16).cuda()
+    q = torch.randn(3, 4, 64, generator=g).to(BF16).cuda()
+    table = torch.randperm(300, generator=g).to(I32).cuda().reshape(3, 100)
+    att, eager = (sm.PagedAttention(3, 4, 2, 64, 16, 100, 300, BF16) for _ in range(2))
+    lens = ints([1, 0, 2])
+    out, lse = att(q, kp, vp, table, lens).clone(), torch.empty(3, 4, device="cuda")
+    torch.cuda.synchronize()
+    cg = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(cg):
+        att(q, kp, vp, table, lens, out=out, lse=lse)
+    for now in ([1600, 0, 777], [0, 0, 0], [3, 1599, 128], [129, 128, 127], [1600, 1600, 1600]):
+        lens.copy_(ints(now))
+        cg.replay()
+        torch.cuda.synchronize()
+        want_lse = torch.empty_like(lse)
+        want = eager(q, kp, vp, table, ints(now), lse=want_lse)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), now
+
+
+def test_results_over_parts_of_a_cache_join_by_their_lse():
+    """The even and the odd pages apart, joined by lse, are the whole."""
+    g = torch.Generator().manual_seed(14)
+    kp, vp = torch.randn(2, 40, 16, 1, 128, generator=g).cuda()
+    q = torch.randn(1, 4, 128, generator=g).cuda()
+    row = torch.randperm(40, generator=g).to(I32).cuda()[None]
+    parts = [sm.PagedAttention(1, 4, 1, 128, 16, n, 40, F32) for n in (40, 20, 20)]
+    lse = [torch.empty(1, 4, device="cuda") for _ in parts]
+    o = [a(q, kp, vp, t.contiguous(), ints([16 * t.shape[1]]), lse=l).double() for a, t, l in zip(parts, (row, row[:, ::2], row[:, 1::2]), lse)]
+    w = torch.softmax(torch.stack(lse[1:]).double(), 0)[..., None]
+    assert (w[0] * o[1] + w[1] * o[2] - o[0]).abs().max() < 2e-5
+    assert (torch.logsumexp(torch.stack(lse[1:]).double(), 0) - lse[0].double()).abs().max() < 1e-5
+
+
+def test_paged_attention_without_requests():
+    att = sm.PagedAttention(0, 4, 2, 64, 16, 4, 8, BF16)
+    kp = torch.zeros(8, 16, 2, 64, dtype=BF16, device="cuda")
+    e = torch.zeros(0, 4, 64, dtype=BF16, device="cuda")
+    assert att(e, kp, kp, torch.zeros(0, 4, dtype=I32, device="cuda"), torch.zeros(0, dtype=I32, device="cuda")).shape == (0, 4, 64)
 
 
 def test_paged_attention_offsets_past_32_bits():
