@@ -80,30 +80,39 @@ int launch_w4_pack(const void* w, const void* scales, const void* zeros, int N, 
 namespace {
 struct W4Args { LinearW4Args a; int blocks, tiles; unsigned mask, offset; };
 
-// One block of one tile: tot += scale (sum over the group of (128 + w) x - (128 + z) sum of x).  keep: 0 takes the block's scales away.
+// sums of x over the groups of a block, in the layout of the products
 template <int MT, int GPB>
-__device__ __forceinline__ void w4_block(const w4_u32x4 wv, const unsigned (&sv)[GPB], const w4_u32x4 (&x)[MT][4], w4_f32x4 (&tot)[MT], unsigned mask, unsigned offset,
-                                         unsigned keep) {
+__device__ __forceinline__ void w4_sums(const w4_u32x4 (&x)[MT][4], w4_f32x4 (&sum)[GPB][MT]) {
   constexpr int STEPS = 4 / GPB;
   const w4_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   const w4_u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
+  for (int i = 0; i < GPB; ++i)
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) sum[i][m] = w4_mfma(x[m][i * STEPS + s], ones, s ? sum[i][m] : zero);
+}
+// One block of one tile: tot += scale (sum over the group of (128 + w) x - (128 + z) sum of x).  keep: 0 takes the block's scales away.
+template <int MT, int GPB>
+__device__ __forceinline__ void w4_block(const w4_u32x4 wv, const unsigned (&sv)[GPB], const w4_u32x4 (&x)[MT][4], const w4_f32x4 (&sum)[GPB][MT], w4_f32x4 (&tot)[MT],
+                                         unsigned mask, unsigned offset, unsigned keep) {
+  constexpr int STEPS = 4 / GPB;
+  const w4_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
   for (int i = 0; i < GPB; ++i) {
-    w4_f32x4 sum[MT], acc[MT];
+    w4_f32x4 acc[MT];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       const w4_u32x4 w = w4_widen(wv[i * STEPS + s], mask, offset);
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        sum[m] = w4_mfma(x[m][i * STEPS + s], ones, s ? sum[m] : zero);
-        acc[m] = w4_mfma(x[m][i * STEPS + s], w, s ? acc[m] : zero);
-      }
+      for (int m = 0; m < MT; ++m) acc[m] = w4_mfma(x[m][i * STEPS + s], w, s ? acc[m] : zero);
     }
     const float scale = __uint_as_float(sv[i] & keep), off = __uint_as_float(sv[i] << 16);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) tot[m][r] = fmaf(scale, fmaf(-off, sum[m][r], acc[m][r]), tot[m][r]);
+      for (int r = 0; r < 4; ++r) tot[m][r] = fmaf(scale, fmaf(-off, sum[i][m][r], acc[m][r]), tot[m][r]);
   }
 }
 
@@ -151,6 +160,7 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
 
   w4_u32x4 x[PB][MT][4], wv[PB][NT];
   unsigned sv[PB][NT][GPB];
+  w4_f32x4 sum[GPB][MT];
   // blocks behind the end read the last one there is, and lose its scales; so do k behind the end, whose scales are zero.
   // A load of x takes 64 k of 8 rows, eight whole lines of memory: the operand's 32 k of 16 rows would be 16 half ones, and lines are what
   // loads are counted in.  Two such loads become two operands when lanes 8 .. 15 of a row of lanes change places with lanes 0 .. 7 of the other.
@@ -202,8 +212,11 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
       for (int i = 0; i < PB; ++i) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          if (n == 0) order_x(i);
-          w4_block<MT, GPB>(wv[i][n], sv[i][n], x[i], tot[n], mask, offset, 0xffff0000u);
+          if (n == 0) {
+            order_x(i);
+            w4_sums<MT, GPB>(x[i], sum);
+          }
+          w4_block<MT, GPB>(wv[i][n], sv[i][n], x[i], sum, tot[n], mask, offset, 0xffff0000u);
           __builtin_amdgcn_sched_barrier(0);
           if (n + 1 == NT) load_x(i, block + TURN + i);
           load_w(i, n, block + TURN + i);
@@ -213,8 +226,9 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       order_x(i);
+      w4_sums<MT, GPB>(x[i], sum);
 #pragma unroll
-      for (int n = 0; n < NT; ++n) w4_block<MT, GPB>(wv[i][n], sv[i][n], x[i], tot[n], mask, offset, block + i < p.blocks ? 0xffff0000u : 0u);
+      for (int n = 0; n < NT; ++n) w4_block<MT, GPB>(wv[i][n], sv[i][n], x[i], sum, tot[n], mask, offset, block + i < p.blocks ? 0xffff0000u : 0u);
     }
   }
 #pragma unroll
