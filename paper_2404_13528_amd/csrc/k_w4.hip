@@ -116,13 +116,6 @@ __device__ __forceinline__ void w4_block(const w4_u32x4 wv, const unsigned (&sv)
   }
 }
 
-__device__ __forceinline__ void w4_store(const LinearW4Args& a, int row, int n, float v) {
-  const int64_t at = (int64_t)row * a.N + n;
-  if (a.bias) v += bf2f(((const bf16_t*)a.bias)[n]);
-  if (a.act) v = gelu_erf(v);
-  if (a.residual) v += bf2f(((const bf16_t*)a.residual)[at]);
-  ((bf16_t*)a.y)[at] = f2bf(v);
-}
 }  // namespace
 
 // A workgroup has NT tiles of 16 features and MT tiles of 16 rows (HALF: up to 8 rows).  Its waves have PB blocks of k each at a time:
@@ -131,12 +124,12 @@ __device__ __forceinline__ void w4_store(const LinearW4Args& a, int row, int n, 
 // waves' sums of a tile meet in LDS.
 // Loads return in the order of their issue, and the compiler's counting of them survives no branch: all loads are unconditional, and their
 // order is pinned.
-// On the GPU, weights cold: 1 x 4096 x 4096 (groups of 128) 4.2 us, 1 x 22016 x 4096 12.9 us (3.7 TB/s), 32 x 22016 x 4096 18.4 us,
-// 32 x 4096 x 11008 14.9 us.
+// On the GPU, weights cold: 1 x 4096 x 4096 (groups of 128) 4.0 us, 1 x 22016 x 4096 12.0 us (4.0 TB/s), 32 x 22016 x 4096 17.5 us,
+// 32 x 4096 x 11008 14.6 us.  Of 17 x 22016 x 4096's 16.6 us the stream of the weights alone takes 11, x 2, the products 3 and the end 1.
 template <int MT, bool HALF, int NT, int GPB, int PB>
 __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
-  constexpr int RT = NT * MT * W4_WAVES <= 96 ? NT : 96 / MT / W4_WAVES;       // tiles that meet at once
-  __shared__ float red[W4_WAVES][RT][MT][16][17];
+  __shared__ float red[W4_WAVES][NT][MT][16][17];
+  __shared__ float s_bias[NT * 16];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   constexpr int ROWS = HALF ? 8 : 16 * MT;
   const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * ROWS, rows = min(ROWS, p.a.M - m0), K = p.a.K;
@@ -197,6 +190,10 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
     for (int j = 0; j < GPB; ++j) sv[i][n][j] = *(const unsigned*)(r + 1024 + j * 64 + c * 4);
     __builtin_amdgcn_sched_barrier(0);
   };
+  if (threadIdx.x < NT * 16) {
+    const int n = tile0 * 16 + threadIdx.x;
+    s_bias[threadIdx.x] = p.a.bias && n < p.a.N ? bf2f(((const bf16_t*)p.a.bias)[n]) : 0.f;
+  }
   constexpr int TURN = W4_WAVES * PB;                  // blocks of a turn: wave w has w * PB ..
   int block = w * PB;
   if (block < p.blocks) {
@@ -231,24 +228,32 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
       for (int n = 0; n < NT; ++n) w4_block<MT, GPB>(wv[i][n], sv[i][n], x[i], sum, tot[n], mask, offset, block + i < p.blocks ? 0xffff0000u : 0u);
     }
   }
+  // the tiles' sums meet: output i is row i / (16 NT), feature i % (16 NT); a thread's residuals are asked for before the waves meet
+  constexpr int OUT = NT * MT * 256, PER = (OUT + 64 * W4_WAVES - 1) / (64 * W4_WAVES);
+  float res[PER];
 #pragma unroll
-  for (int n0 = 0; n0 < NT; n0 += RT) {
-    if (n0) __syncthreads();
+  for (int j = 0; j < PER; ++j) {
+    const int i = threadIdx.x + j * 64 * W4_WAVES, row = i / (16 * NT), n = tile0 * 16 + i % (16 * NT);
+    res[j] = 0.f;
+    if (p.a.residual && row < rows && n < p.a.N) res[j] = bf2f(((const bf16_t*)p.a.residual)[(int64_t)(m0 + row) * p.a.N + n]);
+  }
 #pragma unroll
-    for (int n = 0; n < RT; ++n)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) if (n0 + n < NT) red[w][n][m][4 * g + r][c] = tot[n0 + n < NT ? n0 + n : 0][m][r];
-    __syncthreads();
-    for (int i = threadIdx.x; i < RT * MT * 256; i += 64 * W4_WAVES) {
-      const int f = i % (16 * RT), row = i / (16 * RT), n = (tile0 + n0) * 16 + f;
-      if (row >= rows || n >= p.a.N || n0 + (f >> 4) >= NT) continue;
-      float v = 0.f;
+      for (int r = 0; r < 4; ++r) red[w][n][m][4 * g + r][c] = tot[n][m][r];
+  __syncthreads();
 #pragma unroll
-      for (int u = 0; u < W4_WAVES; ++u) v += red[u][f >> 4][row >> 4][row & 15][f & 15];
-      w4_store(p.a, m0 + row, n, v);
-    }
+  for (int j = 0; j < PER; ++j) {
+    const int i = threadIdx.x + j * 64 * W4_WAVES, row = i / (16 * NT), f = i % (16 * NT), n = tile0 * 16 + f;
+    if (row >= rows || n >= p.a.N) continue;           // (rows <= ROWS: no output behind the last one)
+    float v = 0.f;
+#pragma unroll
+    for (int u = 0; u < W4_WAVES; ++u) v += red[u][f >> 4][row >> 4][row & 15][f & 15];
+    v += s_bias[f];
+    if (p.a.act) v = gelu_erf(v);
+    ((bf16_t*)p.a.y)[(int64_t)(m0 + row) * p.a.N + n] = f2bf(v + res[j]);
   }
 }
 
