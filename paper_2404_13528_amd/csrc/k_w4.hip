@@ -1,8 +1,8 @@
 // Linear with 4-bit weights, group scales and zero points, on few rows: y = act(x W^T + bias) + residual.
 //
-// Bound by the stream of the packed weights (half a byte each, and 4 bytes a group for scale and zero point) and, with many rows, by
-// the x that every workgroup loads (a CU takes in some 45 bytes a ns).  A workgroup has all of K for its 16 to 96 features: its waves
-// take turns over blocks of 128 k and meet in LDS at the end.
+// Bound by the stream of the packed weights (half a byte each, and 4 bytes a group for scale and zero point), with many rows also by the
+// x that every workgroup loads.  A workgroup has all of K for its 16 to 96 features: its waves take turns over blocks of 128 k and meet in
+// LDS at the end.
 //
 //  * The matrix pipe's second operand is 16 features x 32 k: a lane's 8 k of a feature are one 32-bit word, and its four words
 //    of a block one 16-byte load.  Nibble j and j + 4 of a word are the k of a pair: (word >> 4 j) & 0x000f000f with
@@ -155,8 +155,8 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
   unsigned sv[PB][NT][GPB];
   w4_f32x4 sum[GPB][MT];
   // blocks behind the end read the last one there is, and lose its scales; so do k behind the end, whose scales are zero.
-  // A load of x takes 64 k of 8 rows, eight whole lines of memory: the operand's 32 k of 16 rows would be 16 half ones, and lines are what
-  // loads are counted in.  Two such loads become two operands when lanes 8 .. 15 of a row of lanes change places with lanes 0 .. 7 of the other.
+  // A load of x takes 64 k of 8 rows, whole lines of memory.  Two such loads become two operands of 32 k of 16 rows when lanes 8 .. 15 of a row of
+  // lanes change places with lanes 0 .. 7 of the other; up to 8 rows one load is both operands (half the loads and registers).
   auto load_x = [&](int i, int block) {
     block = min(block, p.blocks - 1);
 #pragma unroll
