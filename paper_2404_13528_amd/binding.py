@@ -844,6 +844,16 @@ def _raw_stream(device, stream):
         return torch.cuda.current_stream(device).cuda_stream
 
 
+def _new(shape, dtype, device, stream):
+    """A new tensor for a result: of the current stream, and in use on `stream` if one is given (its memory is not handed out
+    again before that stream is done with it)."""
+    import torch
+    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
 def _dims(t, name, n):
     if getattr(t, "ndim", None) != n:
         raise ValueError("%s must be a tensor of %d axes" % (name, n))
@@ -872,7 +882,7 @@ def page_table(cached, fresh, free_pages, n_free, table, page, n_pages, max_toke
     cfg = _PAGE_CFG.pack(R, page, cols, n_pages, free_cap, max_tokens, table.stride(0) if R > 1 else cols)
     sizes = (R + 1, R, n, n, 1)
     if out is None:
-        whole = torch.empty(2 * (R + n + 1), dtype=i32, device=dev)
+        whole = _new(2 * (R + n + 1), i32, dev, stream)
         at = whole.data_ptr()
         lens = at + 4 * (R + 1)
         pos = lens + 4 * R
@@ -880,7 +890,7 @@ def page_table(cached, fresh, free_pages, n_free, table, page, n_pages, max_toke
     else:
         ptrs = [_flat(t, name, i32, (k,), dev) for t, name, k in zip(out, PageTable._fields, sizes)]
     check(lib().sm_page_table(cfg, *ins, *ptrs, _raw_stream(dev, stream)), "sm_page_table")
-    return PageTable(*whole.split(sizes)) if out is None else out
+    return PageTable(*whole.split_with_sizes(sizes)) if out is None else out
 
 
 class HeadNormRopeDesc(C.Structure):
@@ -914,7 +924,7 @@ def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gam
         hq, shape = heads, (T, heads, d)
         qp = _rows(q, "q", dt, shape, dev)
         if q_out is None:
-            q_out = torch.empty(shape, dtype=dt, device=dev)
+            q_out = _new(shape, dt, dev, stream)
             qo = q_out.data_ptr()
         else:
             qo = _rows(q_out, "q_out", dt, shape, dev)
@@ -927,14 +937,14 @@ def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gam
             out_shape = (n_pages, page, hkv, d)
         if k is not None:
             kp = _rows(k, "k", dt, shape, dev)
-            if k_out is None:
-                k_out = torch.empty(shape, dtype=dt, device=dev)
+            if k_out is None and slots is None:
+                k_out = _new(shape, dt, dev, stream)
             ko = _rows(k_out, "k_out", dt, out_shape, dev)
             ks, kos = k.stride()[:2], k_out.stride()[:-1]
         if v is not None:
             vp = _rows(v, "v", dt, shape, dev)
             if v_out is None and slots is None:
-                v_out = torch.empty(shape, dtype=dt, device=dev)
+                v_out = _new(shape, dt, dev, stream)
             vo = _rows(v_out, "v_out", dt, out_shape, dev)
             vs, vos = v.stride()[:2], v_out.stride()[:-1]
         if slots is None:                         # (row t of a pool of one page)
@@ -980,7 +990,7 @@ class PagedAttention:
         import torch
         c, dt, dev, i32 = self.desc, self.dtype, _device(), torch.int32
         if out is None:
-            out = torch.empty(self.q_shape, dtype=dt, device=dev)
+            out = _new(self.q_shape, dt, dev, stream)
             op = out.data_ptr()
         else:
             op = _rows(out, "out", dt, self.q_shape, dev)
@@ -1027,7 +1037,7 @@ class LinearW4:
         M, _ = _dims(x, "x", 2)
         xp, shape = _flat(x, "x", bf16, (M, self.K), dev), (M, self.N)
         if out is None:
-            out = torch.empty(shape, dtype=bf16, device=dev)
+            out = _new(shape, bf16, dev, stream)
             op = out.data_ptr()
         else:
             op = _flat(out, "out", bf16, shape, dev)

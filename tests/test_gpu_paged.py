@@ -546,6 +546,29 @@ def test_two_objects_on_two_streams():
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
 
 
+def test_results_of_calls_on_a_side_stream():
+    """Outputs that the calls make themselves, on a stream given by the caller: right, and their memory stays theirs while the stream runs."""
+    g = torch.Generator().manual_seed(15)
+    x = torch.randn(5000, 6, 64, generator=g).cuda()
+    gain, pos = torch.ones(64, device="cuda"), torch.arange(5000, dtype=I32, device="cuda")
+    want = sm.head_norm_rope(x, x, x, pos, q_gamma=gain, k_gamma=gain)
+    w, sc = torch.randint(0, 256, (4096, 512), generator=g, dtype=torch.uint8).cuda(), torch.rand(4096, 8, generator=g).to(BF16).cuda()
+    lin, xb = sm.LinearW4(w, sc, group=128), torch.randn(8, 1024, generator=g).to(BF16).cuda()
+    y = lin(xb)
+    one, none, n_free, t = ints([1] * 50), ints([0] * 50), ints([50]), torch.full((50, 3), -1, dtype=I32, device="cuda")
+    free = torch.arange(50, dtype=I32, device="cuda")
+    pt = sm.page_table(none, one, free, n_free, t, 16, 50, 50)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        got = sm.head_norm_rope(x, x, x, pos, q_gamma=gain, k_gamma=gain, stream=side) + (lin(xb, stream=side),) + \
+            tuple(sm.page_table(none, one, free, n_free, t, 16, 50, 50, stream=side))
+        lin(xb, stream=side)                                                        # (dropped at once: its memory is not the next tensor's yet)
+        other = torch.zeros(8, 4096, dtype=BF16, device="cuda")
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want + (y,) + tuple(pt))) and not other.any()
+
+
 def test_binding_refuses_wrong_tensors():
     x = torch.randn(4, 2, 64, device="cuda")
     pos = torch.zeros(4, dtype=I32, device="cuda")
