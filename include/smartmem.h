@@ -473,9 +473,9 @@ int sm_page_table(const sm_page_cfg*, const int32_t* cached, const int32_t* fres
  * (with its output): that part is left out.  Strides: token, head for inputs and q_out; page, token, head for k_out and
  * v_out.  slots null: row t of k_out / v_out is t * stride[1] + head * stride[2].  slots given: k_out / v_out are page
  * pools and row t goes to page slots[t] / page, place slots[t] % page; a slot outside [0, n_pages * page) stores nothing.
- * A token with a negative position is padding: nothing is stored for it.  Two tokens of one slot: each head of
- * the slot holds either of them.  An output may be its input (same address and strides), otherwise they must not overlap.
- * Angles are exact to a 2^-31 revolution at any position.  rot a multiple of twice the 16-byte vector (16 bf16, 8 f32),
+ * A token with a negative position is padding: nothing is stored for it.  Two tokens of one slot: each head of the slot
+ * holds either of them.  An output may be its input (same address and strides), otherwise they must not overlap.
+ * Angles are exact to 2^-27 of a revolution at any position.  rot a multiple of twice the 16-byte vector (16 bf16, 8 f32),
  * d a multiple of the vector, both at most 256; rope_base >= 1; n_pages * page <= 2^30, tokens <= 2^25. */
 typedef struct {
   int32_t dtype, tokens, heads_q, heads_kv, d;
@@ -493,9 +493,9 @@ int sm_head_norm_rope(const sm_head_norm_rope_desc*, const void* q, const void* 
  * multiple of heads_kv).  No token (lens[r] <= 0, or no page of them exists): o = 0, lse = -inf.  lse (nullable)
  * [n_req, heads_q] fp32, contiguous: the natural logarithm of the sum of exp(scale * q . k), with which results over
  * disjoint parts of a cache can be joined.  What lies in a page behind the request's last token is not used, whatever
- * it is.  o must not overlap the inputs.  Strides: request, head (q, o); page, token, head (k_pages, v_pages: token-major [page, token, head, d] and
- * head-major [page, head, token, d] pools alike; page and token strides not negative, a pool's pages within 64 GiB).  The
- * key axis is split over workgroups by the lengths found on the device and joined in fp32.
+ * it is.  o must not overlap the inputs.  Strides: request, head (q, o); page, token, head (k_pages, v_pages: token-major
+ * [page, token, head, d] and head-major [page, head, token, d] pools alike; page and token strides not negative, a pool's
+ * pages within 64 GiB).  The key axis is split over workgroups by the lengths found on the device and joined in fp32.
  * d a multiple of the 16-byte vector (8 bf16, 4 f32), at most 256.  The workspace holds partial results; nothing in it
  * has to survive between calls; calls that share one on different streams race. */
 typedef struct {

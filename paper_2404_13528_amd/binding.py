@@ -1010,6 +1010,7 @@ class LinearW4Desc(C.Structure):
 
 _LINEAR_W4 = struct.Struct("@5i")
 
+
 class LinearW4:
     """sm_linear_w4: a Linear whose weights stay in 4 bits.  w [N, K / 2] uint8 (even k in the low four bits), scales [N, K / group]
     bf16, zeros [N, K / group] uint8 (None: 8), bias [N] bf16 or None.  The weights are packed here, once, into memory of the

@@ -3,8 +3,8 @@
 //
 // A lane has two 16-byte pieces of a head: below `rot` the two halves of its pairs, so that the rotation stays in the lane and an angle
 // serves both, behind it two adjacent pieces.  G lanes make a head, a wave takes 64 / G heads of one token at a time.
-// Angles: position times theta_i / 2 pi as a fraction of 2^64, modulo one revolution, is an integer product, exact at any
-// position; its upper 32 bits go to the sine and cosine (bf16: the hardware's, whose 1e-6 is far below the rounding of the
+// Angles: position times theta_i / 2 pi as a fraction of 2^64, modulo one revolution, is an integer product, which loses
+// nothing at far positions; its upper 32 bits go to the sine and cosine (bf16: the hardware's, whose 1e-6 is far below the rounding of the
 // store; fp32: the library's, in units of pi).
 // Bound by the bytes read and written.
 #include "device_common.h"

@@ -78,8 +78,8 @@ extern "C" int sm_head_norm_rope(const sm_head_norm_rope_desc* c, const void* q,
   if (k) a.part[1] = HeadNormPart{k, c->k_gamma, c->k_beta, k_out, c->k_stride[0], c->k_stride[1], c->k_out_stride[0], c->k_out_stride[1], c->k_out_stride[2], c->heads_kv, 0, 1, paged};
   if (v) a.part[2] = HeadNormPart{v, nullptr, nullptr, v_out, c->v_stride[0], c->v_stride[1], c->v_out_stride[0], c->v_out_stride[1], c->v_out_stride[2], c->heads_kv, 0, 0, paged};
   if (c->rot) {
-    // theta_i / 2 pi in 64 bits behind the point; the long double's 64-bit mantissa loses at most half of the lowest bits to
-    // the repeated product, which a position below 2^31 lifts to less than 2^-25 revolutions' lowest bit
+    // theta_i / 2 pi in 64 bits behind the point.  The repeated product in 64-bit mantissas is off by at most 2 i 2^-64 of theta_i / 2 pi
+    // <= 0.16, with at most 127 factors 2^-58: at positions below 2^31 less than 2^-27 of a revolution
     const long double step = powl((long double)c->rope_base, -2.0L / c->rot);
     long double f = 0.15915494309189533576888376337251436L;
     for (int i = 0; i < c->rot / 2; ++i, f *= step) a.turn[i] = (uint64_t)(f * 18446744073709551616.0L);
