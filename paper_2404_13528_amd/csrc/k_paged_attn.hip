@@ -17,6 +17,8 @@
 //    time, and the weights then carry 16 bits.  Running maximum, sums and O are fp32.
 //  * Keys behind the length and pages outside the pool: their loads go to the pool's first place, their logits become -inf
 //    and their values zero (a NaN there would survive a weight of zero).
+//  * No key with a weight: the sum of the weights is zero (with one it is at least 1), not only the maximum -inf, which it also is if every
+//    logit is NaN, as fmax passes over them; then the sum is NaN, and so is the result.
 #include <algorithm>
 #include "device_common.h"
 #include "paged.h"
@@ -385,8 +387,8 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 && PA_WAVES
       ls = fmaf(f, s_l[i][r], ls);
     }
     if (it.n == 1) {
-      Elem<T>::st((T*)a.o + (int64_t)it.r * a.o_r + (int64_t)(h0 + r) * a.o_h + e, M == -INFINITY ? 0.f : os / ls);
-      if (a.lse && e == 0) a.lse[(int64_t)it.r * a.heads_q + h0 + r] = M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(ls)) * 0.69314718055994531f;
+      Elem<T>::st((T*)a.o + (int64_t)it.r * a.o_r + (int64_t)(h0 + r) * a.o_h + e, ls == 0.f ? 0.f : os / ls);
+      if (a.lse && e == 0) a.lse[(int64_t)it.r * a.heads_q + h0 + r] = ls == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(ls)) * 0.69314718055994531f;
     } else {
       part[r * a.d + e] = os;
       if (e == 0) { part[p.s.rows * a.d + 2 * r] = M; part[p.s.rows * a.d + 2 * r + 1] = ls; }
@@ -448,8 +450,8 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
     for (int x = 0; x < 4; ++x) O[x] = fmaf(f, s_o[i * lg + e][x], O[x]);
   }
   T* out = (T*)a.o + (int64_t)r * a.o_r + (int64_t)h * a.o_h + 4 * e;
-  for (int x = 0; x < 4; ++x) Elem<T>::st(out + x, M == -INFINITY ? 0.f : O[x] / L);
-  if (a.lse && e == 0) a.lse[(int64_t)r * a.heads_q + h] = M == -INFINITY ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994531f;
+  for (int x = 0; x < 4; ++x) Elem<T>::st(out + x, L == 0.f ? 0.f : O[x] / L);
+  if (a.lse && e == 0) a.lse[(int64_t)r * a.heads_q + h] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994531f;
 }
 
 bool paged_attention_fits(int dtype, int n_req, int heads_q, int heads_kv, int d, int64_t max_keys) {

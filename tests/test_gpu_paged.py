@@ -341,6 +341,33 @@ def test_paged_attention_infinite_and_nan_keys_stay_in_their_request(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("n", [1, 200, 300, 5000])
+def test_paged_attention_nan_queries_and_keys_without_weight(n, d, dtype):
+    """A request whose every logit is NaN gives NaN, not the zero of an empty one; keys whose logit is -inf weigh nothing, and where
+    there are no others the request counts as empty."""
+    g = torch.Generator().manual_seed(7)
+    mp = (n + 15) // 16
+    kp, vp = torch.randn(2, 4 * mp, 16, 1, d, generator=g).to(dtype).cuda()
+    q = torch.randn(4, 2, d, generator=g).to(dtype).cuda()
+    q[:, :, 3] = 1.0
+    table = ints(np.arange(4 * mp).reshape(4, mp).tolist())
+    att = sm.PagedAttention(4, 2, 1, d, 16, mp, 4 * mp, dtype)
+    lens = ints([n] * 4)
+    want = att(q, kp, vp, table, lens).clone()
+    q[1, 1] = float("nan")
+    kp[2 * mp:3 * mp, :, :, 3] = float("-inf")
+    kp[3 * mp:].view(-1, d)[:n - 1, 3] = float("-inf")              # the last key alone has a weight
+    lse = torch.empty(4, 2, device="cuda")
+    got = att(q, kp, vp, table, lens, lse=lse)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1, 0], want[1, 0])
+    assert got[1, 1].isnan().all() and lse[1, 1].isnan() and lse[1, 0].isfinite()
+    assert not got[2].any() and (lse[2] == float("-inf")).all()
+    last = vp[3 * mp:].view(-1, d)[n - 1]
+    assert torch.equal(got[3], torch.stack([last, last])) and lse[3].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("R", [64, 65, 256, 257, 1500])
 def test_paged_attention_many_requests(R, dtype):
     """Several requests per lane of the scan that cuts the work, empty ones among them."""
