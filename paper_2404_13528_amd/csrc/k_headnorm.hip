@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void head_norm_rope_kernel(HeadNormArgs a_) {
 #pragma unroll
       for (int e = 0; e < V; ++e) { f0[e] = fmaf(f0[e] * r, g0[e], b0[e]); f1[e] = fmaf(f1[e] * r, g1[e], b1[e]); }
     }
-    if (hv) {
+    if (turns) {                               // (the others' two pieces are no pair: an infinity in one would be a NaN in the other)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float lo = f0[e], hi = f1[e];

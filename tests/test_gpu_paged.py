@@ -233,6 +233,25 @@ def test_head_norm_rope_parts_in_place_and_empty():
     assert not o[0, 0].any() and not o[1, 1].any() and not o[0, 1].isfinite().all() and o[1, 0].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [5, 900])
+@pytest.mark.parametrize("d, rot", [(64, 32), (128, 32), (128, 96), (256, 64), (96, 0)])
+def test_head_norm_rope_features_behind_the_rotation_are_their_own(d, rot, T, dtype):
+    """Without a norm they leave as they came, whatever they are; with one, an infinity gives NaN in its own place and 0 in the others."""
+    g = torch.Generator().manual_seed(d + rot)
+    x = torch.randn(T, 3, d, generator=g).to(dtype).cuda()
+    x[1, 1, rot:] = float("inf")
+    x[2, 0, rot + 3], x[2, 1, d - 1], x[2, 2, d - 9], x[3, 0, rot] = float("nan"), float("-inf"), float("inf"), -0.0
+    pos = torch.arange(T, dtype=I32, device="cuda") + 7
+    clean = x.clone()
+    clean[:, :, rot:] = 0
+    got, want = sm.head_norm_rope(x, None, None, pos, norm="none", rot=rot)[0], sm.head_norm_rope(clean, None, None, pos, norm="none", rot=rot)[0]
+    as_int = torch.int16 if dtype == BF16 else I32
+    assert torch.equal(got[:, :, rot:].contiguous().view(as_int), x[:, :, rot:].contiguous().view(as_int)) and torch.equal(got[:, :, :rot], want[:, :, :rot])
+    o = sm.head_norm_rope(x, None, None, pos, rot=rot, q_gamma=torch.ones(d, dtype=dtype, device="cuda"))[0]
+    assert o[2, 1, d - 1].isnan() and not o[2, 1, :d - 1].any() and o[2, 0].isnan().all()
+
+
 # ------------------------------------------------------------------------------------------------ attention
 
 def attn_case(lens, hq, hkv, d, page, dtype, seed=0, head_major=False, spare_cols=1, q_scale=1.0, scale=None, bad=(), poison=True, values=None):
