@@ -837,6 +837,8 @@ def _device():
 def _raw_stream(device, stream):
     import torch
     if stream is not None:
+        if stream.device != device:
+            raise ValueError("the stream is on %s: a call's tensors and stream belong to the current device, %s" % (stream.device, device))
         return stream.cuda_stream
     try:                                          # (the number alone: a tenth of the time of a Stream object)
         return torch._C._cuda_getCurrentRawStream(device.index)
@@ -845,10 +847,19 @@ def _raw_stream(device, stream):
 
 
 def _new(shape, dtype, device, stream):
-    """A new tensor for a result: of the current stream, and in use on `stream` if one is given (its memory is not handed out
-    again before that stream is done with it)."""
+    """A new tensor for a result: memory of `stream` if one is given (the current stream may still be busy with what it let go), which
+    is not handed out again before the current stream, too, is done with what it had been given until then."""
     import torch
-    t = torch.empty(shape, dtype=dtype, device=device)
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _own(t, stream):
+    """An object's own memory, about to be used on `stream`: if the object goes, it is not handed out before that stream is done."""
     if stream is not None:
         t.record_stream(stream)
     return t
@@ -996,7 +1007,7 @@ class PagedAttention:
             op = _rows(out, "out", dt, self.q_shape, dev)
         args = (_rows(q, "q", dt, self.q_shape, dev), _rows(k_pages, "k_pages", dt, self.pool_shape, dev), _rows(v_pages, "v_pages", dt, self.pool_shape, dev),
                 _rows(table, "table", i32, self.table_shape, dev), _flat(lens, "lens", i32, self.q_shape[:1], dev), op,
-                None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(self.ws, "the workspace", torch.uint8, self.ws.shape, dev))
+                None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(_own(self.ws, stream), "the workspace", torch.uint8, self.ws.shape, dev))
         c.table_pitch = table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1]
         c.q_stride[:], c.o_stride[:] = q.stride()[:2], out.stride()[:2]
         c.k_stride[:], c.v_stride[:] = k_pages.stride()[:3], v_pages.stride()[:3]
@@ -1029,7 +1040,7 @@ class LinearW4:
         if bias is not None:
             _flat(bias, "bias", torch.bfloat16, (N,), dev)
         self.N, self.K, self.group, self.bias = N, 2 * half, group, bias
-        self.packed = torch.empty(n, dtype=u8, device=dev)
+        self.packed = _new(n, u8, dev, stream)
         check(lib().sm_linear_w4_pack(wp, sp, zp, N, self.K, group, self.packed.data_ptr(), _raw_stream(dev, stream)), "sm_linear_w4_pack")
 
     def __call__(self, x, residual=None, act="none", out=None, stream=None):
@@ -1042,8 +1053,8 @@ class LinearW4:
             op = out.data_ptr()
         else:
             op = _flat(out, "out", bf16, shape, dev)
-        check(lib().sm_linear_w4(_LINEAR_W4.pack(M, self.N, self.K, self.group, ACT[act]), xp, _flat(self.packed, "the packed weights", torch.uint8, self.packed.shape, dev),
-                                 None if self.bias is None else self.bias.data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev),
+        check(lib().sm_linear_w4(_LINEAR_W4.pack(M, self.N, self.K, self.group, ACT[act]), xp, _flat(_own(self.packed, stream), "the packed weights", torch.uint8, self.packed.shape, dev),
+                                 None if self.bias is None else _own(self.bias, stream).data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev),
                                  op, _raw_stream(dev, stream)), "sm_linear_w4")
         return out
 

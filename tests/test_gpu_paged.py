@@ -615,6 +615,29 @@ def test_results_of_calls_on_a_side_stream():
         assert all(torch.equal(a, b) for a, b in zip(got, want + (y,) + tuple(pt))) and not other.any()
 
 
+def test_results_of_calls_on_a_side_stream_take_its_own_memory():
+    """Memory that the current stream has just let go may still be in use there: what a call makes for another stream is not put into it."""
+    x, pos, gain = torch.randn(5000, 6, 64, device="cuda"), torch.arange(5000, dtype=I32, device="cuda"), torch.ones(64, device="cuda")
+    w, sc = torch.zeros(4096, 512, dtype=torch.uint8, device="cuda"), torch.ones(4096, 8, dtype=BF16, device="cuda")
+    xb, side = torch.randn(1000, 1024, device="cuda").to(BF16), torch.cuda.Stream()
+    lin, q = sm.LinearW4(w, sc), torch.randn(16, 256, 64, device="cuda").to(BF16)
+    att, kp, t = sm.PagedAttention(16, 256, 1, 64, 16, 1, 4, BF16), torch.randn(4, 16, 1, 64, device="cuda").to(BF16), torch.zeros(16, 1, dtype=I32, device="cuda")
+    one = torch.zeros(1, dtype=I32, device="cuda")
+    calls = {"norm": lambda s: sm.head_norm_rope(x, None, None, pos, q_gamma=gain, stream=s)[0], "linear": lambda s: lin(xb, stream=s),
+             "attention": lambda s: att(q, kp, kp, t, t[:, 0].contiguous(), stream=s), "pack": lambda s: sm.LinearW4(w, sc, stream=s).packed,
+             "pages": lambda s: sm.page_table(one, one, one, one, t[:1], 16, 4, 500000, stream=s).starts}
+    for name, call in calls.items():
+        for _ in range(3):
+            r = call(None)
+            torch.cuda.synchronize()
+            span = (r.untyped_storage().data_ptr(), r.untyped_storage().nbytes())
+            del r                                                                   # (the next call of this size on this stream would get it)
+            r = call(side).untyped_storage()
+            side.synchronize()
+            apart = r.data_ptr() >= span[0] + span[1] or span[0] >= r.data_ptr() + r.nbytes()
+            assert apart, name
+
+
 def test_binding_refuses_wrong_tensors():
     x = torch.randn(4, 2, 64, device="cuda")
     pos = torch.zeros(4, dtype=I32, device="cuda")

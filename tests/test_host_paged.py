@@ -160,3 +160,11 @@ def test_binding_refuses_host_tensors():
         sm.head_norm_rope(None, None, None, i32)
     with pytest.raises(ValueError):
         sm.LinearW4(torch.zeros(8, 16, dtype=torch.uint8), torch.zeros(8, 1, dtype=torch.bfloat16), group=32)
+
+
+def test_binding_refuses_a_stream_of_another_device():
+    class Stream:
+        device, cuda_stream = torch.device("cuda", 1), 5
+    assert sm._raw_stream(torch.device("cuda", 1), Stream) == 5
+    with pytest.raises(ValueError, match="stream is on cuda:1"):
+        sm._raw_stream(torch.device("cuda", 0), Stream)
