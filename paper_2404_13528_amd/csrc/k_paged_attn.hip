@@ -33,6 +33,9 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 pa_bf16x8;
 
 constexpr int PA_ROWS = 16;               // query heads a workgroup serves at once
 constexpr int PA_UNIT = 128;              // keys: chunks are whole units
+// The weights go to their product with the values as multiples of this, so that a sum of 2^24 values of any finite size is finite.  Every wave and
+// chunk sums by its own maximum: without it large values of keys that weigh nothing beside another chunk's would be infinite there.
+constexpr float PA_LOW = 0x1p-24f;
 
 // How the work is cut.  A chunk's start costs some 4 us (lengths, page table, first keys: three trips to memory), so at first there are as
 // many chunks as two workgroups a CU (heads over 128: one): 64 requests of 1000 keys take 54 us, with twice as many chunks 62.  But where
@@ -269,7 +272,7 @@ __device__ __forceinline__ void pa_values(PaTile<T, DP>& t, float* s, const unsi
   }
   float p[NV];
 #pragma unroll
-  for (int i = 0; i < NV; ++i) { p[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += p[i]; }
+  for (int i = 0; i < NV; ++i) { p[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += p[i]; p[i] *= PA_LOW; }
   if constexpr (sizeof(T) == 2) {
     // the rest is never negative, and kept above zero, so that an infinite value keeps its sign: 0 x inf is no number
     pa_u32x4 hi;
@@ -387,7 +390,7 @@ __global__ __launch_bounds__(64 * PA_WAVES, DP == 64 ? 4 : DP == 128 && PA_WAVES
       ls = fmaf(f, s_l[i][r], ls);
     }
     if (it.n == 1) {
-      Elem<T>::st((T*)a.o + (int64_t)it.r * a.o_r + (int64_t)(h0 + r) * a.o_h + e, ls == 0.f ? 0.f : os / ls);
+      Elem<T>::st((T*)a.o + (int64_t)it.r * a.o_r + (int64_t)(h0 + r) * a.o_h + e, ls == 0.f ? 0.f : os / ls * (1.f / PA_LOW));
       if (a.lse && e == 0) a.lse[(int64_t)it.r * a.heads_q + h0 + r] = ls == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(ls)) * 0.69314718055994531f;
     } else {
       part[r * a.d + e] = os;
@@ -450,7 +453,7 @@ __global__ __launch_bounds__(256) void paged_attn_join_kernel(PaArgs p) {
     for (int x = 0; x < 4; ++x) O[x] = fmaf(f, s_o[i * lg + e][x], O[x]);
   }
   T* out = (T*)a.o + (int64_t)r * a.o_r + (int64_t)h * a.o_h + 4 * e;
-  for (int x = 0; x < 4; ++x) Elem<T>::st(out + x, L == 0.f ? 0.f : O[x] / L);
+  for (int x = 0; x < 4; ++x) Elem<T>::st(out + x, L == 0.f ? 0.f : O[x] / L * (1.f / PA_LOW));
   if (a.lse && e == 0) a.lse[(int64_t)r * a.heads_q + h] = L == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(L)) * 0.69314718055994531f;
 }
 

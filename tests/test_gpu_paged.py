@@ -386,6 +386,38 @@ def test_paged_attention_nan_queries_and_keys_without_weight(n, d, dtype):
     assert torch.equal(got[3], torch.stack([last, last])) and lse[3].isfinite().all()
 
 
+@pytest.mark.parametrize("dtype", [F32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n", [2, 200, 1000])
+def test_paged_attention_largest_values_of_keys_without_weight(n, d, dtype):
+    """A key whose weight is zero (e^-256 of the first one's) adds nothing, however large its finite value is."""
+    mp = (n + 15) // 16
+    kp, vp = torch.zeros(2, mp, 16, 1, d, dtype=dtype, device="cuda")
+    kp.view(-1, d)[1:, 0] = -256.0
+    vp.view(-1, d)[1:] = torch.finfo(dtype).max
+    vp.view(-1, d)[2::2] *= -1
+    vp.view(-1, d)[0] = 1.5
+    q = torch.zeros(1, 2, d, dtype=dtype, device="cuda")
+    q[:, :, 0] = 1.0
+    got = sm.PagedAttention(1, 2, 1, d, 16, mp, mp, dtype, scale=1.0)(q, kp, vp, torch.arange(mp, dtype=I32, device="cuda")[None], ints([n]))
+    assert (got == 1.5).all(), got.unique().tolist()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("n", [2, 200, 1000, 20000])
+def test_paged_attention_values_whose_sum_is_no_float(n, d, dtype):
+    """n equal weights on n values of half the type's largest: the mean is that value, which no rounding on the way leaves by more than
+    (n / 16 + 64) 2^-24 (the blocks of the sums), though n times it is past the largest fp32 number."""
+    mp = (n + 15) // 16
+    kp, vp = torch.zeros(2, mp, 16, 1, d, dtype=dtype, device="cuda")
+    vp.view(-1, d)[:n] = torch.finfo(dtype).max / 2
+    q = torch.zeros(1, 2, d, dtype=dtype, device="cuda")
+    got = sm.PagedAttention(1, 2, 1, d, 16, mp, mp, dtype)(q, kp, vp, torch.arange(mp, dtype=I32, device="cuda")[None], ints([n]))
+    want = vp[0, 0, 0, 0].double()
+    assert (got.double() / want - 1).abs().max() <= HALF[dtype] + (n / 16 + 64) * 2.0 ** -24
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("R", [64, 65, 256, 257, 1500])
 def test_paged_attention_many_requests(R, dtype):
