@@ -274,11 +274,16 @@ __device__ __forceinline__ void pa_values(PaTile<T, DP>& t, float* s, const unsi
 #pragma unroll
   for (int i = 0; i < NV; ++i) { p[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += p[i]; p[i] *= PA_LOW; }
   if constexpr (sizeof(T) == 2) {
-    // the rest is never negative, and kept above zero, so that an infinite value keeps its sign: 0 x inf is no number
+    // Both terms are above zero wherever the weight is (down to 2^-90), so that an infinite value keeps its sign: 0 x inf is no number.  What the
+    // first term leaves is at least 2^-12 of the weight, and nothing where the weight is zero.
     pa_u32x4 hi;
     float rest[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rest[i] = fmaxf(p[i] - __uint_as_float(__float_as_uint(p[i]) & 0xffff0000u), 1e-37f);
+    for (int i = 0; i < 8; ++i) {
+      const unsigned top = __float_as_uint(p[i] * (1.f - 0x1p-12f));
+      rest[i] = p[i] - __uint_as_float(top & 0xffff0000u);
+      p[i] = __uint_as_float(top);
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) hi[e] = __builtin_amdgcn_perm(__float_as_uint(p[2 * e + 1]), __float_as_uint(p[2 * e]), 0x07060302u);
     const pa_u32x4 lo = pack8(rest);

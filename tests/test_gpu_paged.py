@@ -386,7 +386,7 @@ def test_paged_attention_nan_queries_and_keys_without_weight(n, d, dtype):
     assert torch.equal(got[3], torch.stack([last, last])) and lse[3].isfinite().all()
 
 
-@pytest.mark.parametrize("dtype", [F32])
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("n", [2, 200, 1000])
 def test_paged_attention_largest_values_of_keys_without_weight(n, d, dtype):
