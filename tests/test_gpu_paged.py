@@ -419,6 +419,22 @@ def test_paged_attention_values_whose_sum_is_no_float(n, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_paged_attention_weights_carry_fp32(d, dtype):
+    """Two keys with values 1 and -1 and logits 0 and -x: the result is tanh(x / 2), a difference of weights near 1 that shows what each of
+    them has lost.  The smaller weight comes from its logit times log2 e and an exponential of one unit in the last place (2^-24 both, as
+    x < 2^-10), and may lose 2^-23 when it is split; the larger is 1.  Half of that error is the result's: 2^-23, then the store."""
+    x = (torch.arange(129, 257, 2).view(4, 16) * 2.0 ** -19).to(dtype).cuda()              # (eight bits: a bf16 each; bits down to 2^-19 in the weight)
+    q = torch.zeros(4, 16, d, dtype=dtype, device="cuda")
+    q[:, :, 0] = x
+    kp, vp = torch.zeros(2, 1, 16, 1, d, dtype=dtype, device="cuda")
+    kp[0, 1, 0, 0], vp[0, 0], vp[0, 1] = -1.0, 1.0, -1.0
+    got = sm.PagedAttention(4, 16, 1, d, 16, 1, 1, dtype, scale=1.0)(q, kp, vp, ints([[0]] * 4), ints([2] * 4))
+    want = torch.tanh(x.double() / 2)[..., None].expand(4, 16, d)
+    check(got, to_np(want), HALF[dtype] * np.abs(to_np(want)) + 2.0 ** -23, "o")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("R", [64, 65, 256, 257, 1500])
 def test_paged_attention_many_requests(R, dtype):
     """Several requests per lane of the scan that cuts the work, empty ones among them."""
