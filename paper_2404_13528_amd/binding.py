@@ -976,6 +976,9 @@ class PagedAttentionDesc(C.Structure):
                [("table_pitch", C.c_int64)] + [(n, C.c_int64 * 2) for n in ("q_stride", "o_stride")] + [(n, C.c_int64 * 3) for n in ("k_stride", "v_stride")]
 
 
+_PAGED_ATTENTION = struct.Struct("@8ifq4q6q")             # PagedAttentionDesc in one step
+
+
 class PagedAttention:
     """sm_paged_attention; owns its workspace.  q [n_req, heads_q, d], k_pages / v_pages [n_pages, page, heads_kv, d] (strided views: a
     head-major pool is passed permuted), table [n_req, max_pages] and lens [n_req] int32 -> o [n_req, heads_q, d]; lse: a contiguous
@@ -985,13 +988,10 @@ class PagedAttention:
         import torch
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError("unsupported dtype %s" % dtype)
-        c = PagedAttentionDesc()
-        c.dtype = SM_F32 if dtype == torch.float32 else SM_BF16
-        c.n_req, c.heads_q, c.heads_kv, c.d, c.page, c.max_pages, c.n_pages = n_req, heads_q, heads_kv, d, page, max_pages, n_pages
-        c.scale = d ** -0.5 if scale is None else scale
-        c.table_pitch = max_pages
-        self.desc, self.dtype = c, dtype
-        n = lib().sm_paged_attention_workspace_bytes(C.byref(c))
+        # (what stays the same from call to call; strides and pitch belong to a call, which packs a descriptor of its own)
+        self.sizes = (SM_F32 if dtype == torch.float32 else SM_BF16, n_req, heads_q, heads_kv, d, page, max_pages, n_pages, d ** -0.5 if scale is None else scale)
+        self.dtype = dtype
+        n = lib().sm_paged_attention_workspace_bytes(_PAGED_ATTENTION.pack(*self.sizes, max_pages, *[0] * 10))
         if n == 0:
             raise SmError("sm_paged_attention_workspace_bytes: " + lib().sm_last_error().decode())
         self.ws = torch.empty(n, dtype=torch.uint8, device="cuda")
@@ -999,7 +999,7 @@ class PagedAttention:
 
     def __call__(self, q, k_pages, v_pages, table, lens, out=None, lse=None, stream=None):
         import torch
-        c, dt, dev, i32 = self.desc, self.dtype, _device(), torch.int32
+        dt, dev, i32 = self.dtype, _device(), torch.int32
         if out is None:
             out = _new(self.q_shape, dt, dev, stream)
             op = out.data_ptr()
@@ -1008,10 +1008,9 @@ class PagedAttention:
         args = (_rows(q, "q", dt, self.q_shape, dev), _rows(k_pages, "k_pages", dt, self.pool_shape, dev), _rows(v_pages, "v_pages", dt, self.pool_shape, dev),
                 _rows(table, "table", i32, self.table_shape, dev), _flat(lens, "lens", i32, self.q_shape[:1], dev), op,
                 None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(_own(self.ws, stream), "the workspace", torch.uint8, self.ws.shape, dev))
-        c.table_pitch = table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1]
-        c.q_stride[:], c.o_stride[:] = q.stride()[:2], out.stride()[:2]
-        c.k_stride[:], c.v_stride[:] = k_pages.stride()[:3], v_pages.stride()[:3]
-        check(lib().sm_paged_attention(C.byref(c), *args, self.ws.numel(), _raw_stream(dev, stream)), "sm_paged_attention")
+        desc = _PAGED_ATTENTION.pack(*self.sizes, table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1], *q.stride()[:2], *out.stride()[:2],
+                                     *k_pages.stride()[:3], *v_pages.stride()[:3])
+        check(lib().sm_paged_attention(desc, *args, self.ws.numel(), _raw_stream(dev, stream)), "sm_paged_attention")
         return out
 
 

@@ -1,6 +1,8 @@
 """Host side of the paged-cache operators and the 4-bit Linear without a GPU: what is refused, and that it is refused before any
 pointer is looked at (the pointers here are made up)."""
 import ctypes as C
+import sys
+import threading
 
 import pytest
 import torch
@@ -168,3 +170,72 @@ def test_binding_refuses_a_stream_of_another_device():
     assert sm._raw_stream(torch.device("cuda", 1), Stream) == 5
     with pytest.raises(ValueError, match="stream is on cuda:1"):
         sm._raw_stream(torch.device("cuda", 0), Stream)
+
+
+def without_gpu(monkeypatch, **calls):
+    """The binding with host tensors and Python functions in the library's place."""
+    class Lib:
+        sm_paged_attention_workspace_bytes = staticmethod(lambda desc: 256)
+    for name, f in calls.items():
+        setattr(Lib, name, staticmethod(f))
+    monkeypatch.setattr(sm, "lib", lambda: Lib)
+    monkeypatch.setattr(sm, "_device", lambda: torch.device("cpu"))
+    monkeypatch.setattr(sm, "_raw_stream", lambda device, stream: 0)
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: empty(*a, **{**kw, "device": "cpu"}))
+
+
+def in_threads(*calls, n):
+    """Every call n times in a thread of its own, changing threads as often as Python can."""
+    errors = []
+
+    def run(call):
+        try:
+            for _ in range(n):
+                call()
+        except BaseException as e:
+            errors.append(e)
+    before = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        threads = [threading.Thread(target=run, args=(c,)) for c in calls]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        sys.setswitchinterval(before)
+    assert not errors, errors[:3]
+
+
+def paged_attention_calls(att):
+    """Two calls that differ in every stride."""
+    q, wide = torch.zeros(4, 8, 64), torch.zeros(4, 16, 128)[:, ::2, :64]
+    kp, vp = torch.zeros(6, 16, 2, 64), torch.zeros(6, 2, 16, 128)[..., :64].transpose(1, 2)
+    table, lens = torch.zeros(4, 8, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    roomy = torch.zeros(4, 32, dtype=torch.int32)[:, :8]
+    out, strided = torch.zeros(4, 8, 64), torch.zeros(4, 8, 96)[..., :64]
+    return lambda: att(q, kp, kp, table, lens, out=out), lambda: att(wide, vp, vp, roomy, lens, out=strided)
+
+
+def test_paged_attention_from_two_threads_has_the_strides_of_its_own_call(monkeypatch):
+    seen, wrong = {}, []
+
+    def call(desc, q, *rest):
+        d = C.cast(desc, C.POINTER(sm.PagedAttentionDesc)).contents
+        strides = (d.table_pitch, *d.q_stride, *d.o_stride, *d.k_stride, *d.v_stride)
+        if seen.setdefault(q, strides) != strides:
+            wrong.append(strides)
+        return 0
+    without_gpu(monkeypatch, sm_paged_attention=call)
+    a, b = paged_attention_calls(sm.PagedAttention(4, 8, 2, 64, 16, 8, 6, torch.float32))
+    a()
+    b()
+    assert sorted(seen.values()) == [(8, 512, 64, 512, 64, 2048, 128, 64, 2048, 128, 64), (32, 2048, 256, 768, 96, 4096, 128, 2048, 4096, 128, 2048)]
+    in_threads(a, b, n=5000)
+    assert not wrong, (len(wrong), wrong[0])
+
+
+def test_packed_descriptors_are_the_structures():
+    for packed, desc in ((sm._PAGE_CFG, sm.PageCfg), (sm._HEAD_NORM_ROPE, sm.HeadNormRopeDesc), (sm._PAGED_ATTENTION, sm.PagedAttentionDesc), (sm._LINEAR_W4, sm.LinearW4Desc)):
+        assert packed.size == C.sizeof(desc)
