@@ -9,6 +9,7 @@ import collections
 import ctypes as C
 import os
 import struct
+import threading
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsmartmem.so")
@@ -982,7 +983,8 @@ _PAGED_ATTENTION = struct.Struct("@8ifq4q6q")             # PagedAttentionDesc i
 class PagedAttention:
     """sm_paged_attention; owns its workspace.  q [n_req, heads_q, d], k_pages / v_pages [n_pages, page, heads_kv, d] (strided views: a
     head-major pool is passed permuted), table [n_req, max_pages] and lens [n_req] int32 -> o [n_req, heads_q, d]; lse: a contiguous
-    fp32 [n_req, heads_q] to fill with the logarithm of the softmax sums.  Calls of one object on different streams race."""
+    fp32 [n_req, heads_q] to fill with the logarithm of the softmax sums.  Threads may share an object on one stream; calls on different
+    streams (and replays of graphs that captured them) share its workspace and have to be kept apart by the caller."""
 
     def __init__(self, n_req, heads_q, heads_kv, d, page, max_pages, n_pages, dtype, scale=None):
         import torch
@@ -990,7 +992,7 @@ class PagedAttention:
             raise TypeError("unsupported dtype %s" % dtype)
         # (what stays the same from call to call; strides and pitch belong to a call, which packs a descriptor of its own)
         self.sizes = (SM_F32 if dtype == torch.float32 else SM_BF16, n_req, heads_q, heads_kv, d, page, max_pages, n_pages, d ** -0.5 if scale is None else scale)
-        self.dtype = dtype
+        self.dtype, self._one = dtype, threading.Lock()
         n = lib().sm_paged_attention_workspace_bytes(_PAGED_ATTENTION.pack(*self.sizes, max_pages, *[0] * 10))
         if n == 0:
             raise SmError("sm_paged_attention_workspace_bytes: " + lib().sm_last_error().decode())
@@ -1010,7 +1012,9 @@ class PagedAttention:
                 None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(_own(self.ws, stream), "the workspace", torch.uint8, self.ws.shape, dev))
         desc = _PAGED_ATTENTION.pack(*self.sizes, table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1], *q.stride()[:2], *out.stride()[:2],
                                      *k_pages.stride()[:3], *v_pages.stride()[:3])
-        check(lib().sm_paged_attention(desc, *args, self.ws.numel(), _raw_stream(dev, stream)), "sm_paged_attention")
+        raw = _raw_stream(dev, stream)
+        with self._one:                           # (a call's two kernels follow each other in the stream)
+            check(lib().sm_paged_attention(desc, *args, self.ws.numel(), raw), "sm_paged_attention")
         return out
 
 

@@ -9,6 +9,8 @@ fp32 (the library's), times the pair.
 Attention: a logit's error is below (d + 4) 2^-24 of sum |q k| * |scale| (products exact in bf16, sums in fp32), and moves a weight by
 that much, numerator and denominator; the weights themselves carry 2^-16 (bf16: two terms of 8 bits each) resp. 2^-22, and sums of up
 to n keys in blocks (n / 16 + 64) 2^-24 of sum p |v|."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -638,6 +640,31 @@ def test_two_objects_on_two_streams():
             atts[i](q[i], kp, vp, table, lens, out=outs[i], stream=streams[i])
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_one_object_from_two_threads():
+    """One stream, one workspace, split requests: each thread's queries and results with strides of their own."""
+    g = torch.Generator().manual_seed(16)
+    kp, vp = torch.randn(2, 512, 16, 2, 128, generator=g).to(BF16).cuda()
+    table = torch.randperm(512, generator=g).to(I32).cuda().reshape(2, 256)
+    att, lens = sm.PagedAttention(2, 8, 2, 128, 16, 256, 512, BF16), [ints([4096, 4000]), ints([300, 3000])]
+    q = [torch.randn(2, 8, 128, generator=g).to(BF16).cuda(), torch.randn(2, 9, 256, generator=g).to(BF16).cuda()[:, 1:, :128]]
+    out = [torch.empty(2, 8, 128, dtype=BF16, device="cuda"), torch.empty(2, 8, 136, dtype=BF16, device="cuda")[..., :128]]
+    want = [att(q[i], kp, vp, table, lens[i]).clone() for i in range(2)]
+    torch.cuda.synchronize()
+    off = []
+
+    def run(i):
+        for _ in range(100):
+            out[i].zero_()
+            att(q[i], kp, vp, table, lens[i], out=out[i])
+            off.append(not torch.equal(out[i], want[i]))
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(off) == 200 and not any(off)
 
 
 def test_results_of_calls_on_a_side_stream():

@@ -239,3 +239,18 @@ def test_paged_attention_from_two_threads_has_the_strides_of_its_own_call(monkey
 def test_packed_descriptors_are_the_structures():
     for packed, desc in ((sm._PAGE_CFG, sm.PageCfg), (sm._HEAD_NORM_ROPE, sm.HeadNormRopeDesc), (sm._PAGED_ATTENTION, sm.PagedAttentionDesc), (sm._LINEAR_W4, sm.LinearW4Desc)):
         assert packed.size == C.sizeof(desc)
+
+
+def test_paged_attention_from_two_threads_one_call_at_a_time(monkeypatch):
+    """The two kernels of a call share the object's workspace: no other call's may come between them in the stream."""
+    inside, met = [0], []
+
+    def call(*args):
+        inside[0] += 1
+        for _ in range(20):                                          # (time for the other thread, as the C call gives it)
+            met.append(inside[0])
+        inside[0] -= 1
+        return 0
+    without_gpu(monkeypatch, sm_paged_attention=call)
+    in_threads(*paged_attention_calls(sm.PagedAttention(4, 8, 2, 64, 16, 8, 6, torch.float32)), n=1000)
+    assert max(met) == 1
