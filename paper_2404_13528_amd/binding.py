@@ -859,11 +859,38 @@ def _new(shape, dtype, device, stream):
     return t
 
 
-def _own(t, stream):
-    """An object's own memory, about to be used on `stream`: if the object goes, it is not handed out before that stream is done."""
-    if stream is not None:
-        t.record_stream(stream)
-    return t
+class _Kept:
+    """Device memory that an object keeps from call to call.  It is made on one stream, where work on what lay there before may be pending and a kernel
+    may be filling it, and used on any: a stream's first call waits for that, and if the object goes, the memory is not handed out again
+    before the streams that used it are done."""
+
+    def __init__(self, device, stream, *tensors):
+        import torch
+        s = torch.cuda.current_stream(device) if stream is None else stream
+        self.tensors, self.streams = tensors, {s.cuda_stream}
+        for t in tensors:                         # (one that the caller made may be of another stream)
+            t.record_stream(s)
+        self.made = None if _capturing(s) else s.record_event()
+
+    def used_on(self, device, stream):
+        """The number of the stream of a call that is about to use the memory."""
+        import torch
+        raw = _raw_stream(device, stream)
+        if raw not in self.streams:
+            s = torch.cuda.current_stream(device) if stream is None else stream
+            for t in self.tensors:
+                t.record_stream(s)
+            if not _capturing(s):                 # (a captured stream waits for nothing outside its graph; torch.cuda.graph waits for the device first)
+                if self.made is not None:
+                    s.wait_event(self.made)
+                self.streams.add(raw)
+        return raw
+
+
+def _capturing(stream):
+    import torch
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
 
 
 def _dims(t, name, n):
@@ -984,7 +1011,7 @@ class PagedAttention:
     """sm_paged_attention; owns its workspace.  q [n_req, heads_q, d], k_pages / v_pages [n_pages, page, heads_kv, d] (strided views: a
     head-major pool is passed permuted), table [n_req, max_pages] and lens [n_req] int32 -> o [n_req, heads_q, d]; lse: a contiguous
     fp32 [n_req, heads_q] to fill with the logarithm of the softmax sums.  Threads may share an object on one stream; calls on different
-    streams (and replays of graphs that captured them) share its workspace and have to be kept apart by the caller."""
+    streams (and replays of graphs that captured them, for which the object has to live on) share its workspace and have to be kept apart by the caller."""
 
     def __init__(self, n_req, heads_q, heads_kv, d, page, max_pages, n_pages, dtype, scale=None):
         import torch
@@ -996,7 +1023,9 @@ class PagedAttention:
         n = lib().sm_paged_attention_workspace_bytes(_PAGED_ATTENTION.pack(*self.sizes, max_pages, *[0] * 10))
         if n == 0:
             raise SmError("sm_paged_attention_workspace_bytes: " + lib().sm_last_error().decode())
-        self.ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        dev = _device()
+        self.ws = _new(n, torch.uint8, dev, None)
+        self._kept = _Kept(dev, None, self.ws)
         self.q_shape, self.pool_shape, self.table_shape = (n_req, heads_q, d), (n_pages, page, heads_kv, d), (n_req, max_pages)
 
     def __call__(self, q, k_pages, v_pages, table, lens, out=None, lse=None, stream=None):
@@ -1009,10 +1038,10 @@ class PagedAttention:
             op = _rows(out, "out", dt, self.q_shape, dev)
         args = (_rows(q, "q", dt, self.q_shape, dev), _rows(k_pages, "k_pages", dt, self.pool_shape, dev), _rows(v_pages, "v_pages", dt, self.pool_shape, dev),
                 _rows(table, "table", i32, self.table_shape, dev), _flat(lens, "lens", i32, self.q_shape[:1], dev), op,
-                None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(_own(self.ws, stream), "the workspace", torch.uint8, self.ws.shape, dev))
+                None if lse is None else _flat(lse, "lse", torch.float32, self.q_shape[:2], dev), _flat(self.ws, "the workspace", torch.uint8, self.ws.shape, dev))
         desc = _PAGED_ATTENTION.pack(*self.sizes, table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1], *q.stride()[:2], *out.stride()[:2],
                                      *k_pages.stride()[:3], *v_pages.stride()[:3])
-        raw = _raw_stream(dev, stream)
+        raw = self._kept.used_on(dev, stream)
         with self._one:                           # (a call's two kernels follow each other in the stream)
             check(lib().sm_paged_attention(desc, *args, self.ws.numel(), raw), "sm_paged_attention")
         return out
@@ -1045,6 +1074,7 @@ class LinearW4:
         self.N, self.K, self.group, self.bias = N, 2 * half, group, bias
         self.packed = _new(n, u8, dev, stream)
         check(lib().sm_linear_w4_pack(wp, sp, zp, N, self.K, group, self.packed.data_ptr(), _raw_stream(dev, stream)), "sm_linear_w4_pack")
+        self._kept = _Kept(dev, stream, self.packed, *(() if bias is None else (bias,)))
 
     def __call__(self, x, residual=None, act="none", out=None, stream=None):
         import torch
@@ -1056,9 +1086,9 @@ class LinearW4:
             op = out.data_ptr()
         else:
             op = _flat(out, "out", bf16, shape, dev)
-        check(lib().sm_linear_w4(_LINEAR_W4.pack(M, self.N, self.K, self.group, ACT[act]), xp, _flat(_own(self.packed, stream), "the packed weights", torch.uint8, self.packed.shape, dev),
-                                 None if self.bias is None else _own(self.bias, stream).data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev),
-                                 op, _raw_stream(dev, stream)), "sm_linear_w4")
+        check(lib().sm_linear_w4(_LINEAR_W4.pack(M, self.N, self.K, self.group, ACT[act]), xp, _flat(self.packed, "the packed weights", torch.uint8, self.packed.shape, dev),
+                                 None if self.bias is None else self.bias.data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev),
+                                 op, self._kept.used_on(dev, stream)), "sm_linear_w4")
         return out
 
 

@@ -713,6 +713,78 @@ def test_results_of_calls_on_a_side_stream_take_its_own_memory():
             assert apart, name
 
 
+def busy(n):
+    """Work of some milliseconds on the current stream that ends in n bytes of ones; their memory is let go at once."""
+    a = torch.randn(4096, 4096, device="cuda")
+    b = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for _ in range(10):
+        a = a @ a * 0.01
+    b.copy_((a.flatten()[:1] != 12345.0).to(torch.uint8).expand(n))
+    return b.data_ptr()
+
+
+def attention_and_linear():
+    """name -> (make the object, call it, its memory), on inputs that are ready."""
+    g = torch.Generator().manual_seed(17)
+    kp, vp = torch.randn(2, 512, 16, 2, 128, generator=g).to(BF16).cuda()
+    q, lens = torch.randn(2, 8, 128, generator=g).to(BF16).cuda(), ints([4096, 4000])
+    table = torch.randperm(512, generator=g).to(I32).cuda().reshape(2, 256)
+    w, sc = torch.randint(0, 256, (8192, 2048), generator=g, dtype=torch.uint8).cuda(), torch.rand(8192, 32, generator=g).to(BF16).cuda()
+    x, bias = torch.randn(8, 4096, generator=g).to(BF16).cuda(), torch.randn(8192, generator=g).to(BF16).cuda()
+    return {"attention": (lambda: sm.PagedAttention(2, 8, 2, 128, 16, 256, 512, BF16), lambda o, **kw: o(q, kp, vp, table, lens, **kw), lambda o: o.ws),
+            "linear": (lambda: sm.LinearW4(w, sc, bias=bias), lambda o, **kw: o(x, **kw), lambda o: o.packed)}
+
+
+@pytest.mark.parametrize("name", ["attention", "linear"])
+@pytest.mark.parametrize("given", [True, False])
+def test_objects_made_on_a_busy_stream_and_called_on_another(name, given):
+    """The object's memory is that of a tensor which the current stream has still to fill; the first call goes to another stream at once."""
+    make, call, memory = attention_and_linear()[name]
+    side = torch.cuda.Stream()
+    first = make()
+    n = memory(first).numel()
+    want = call(first).clone()
+    torch.cuda.synchronize()
+    held, same = [], 0
+    for _ in range(3):
+        at = busy(n)
+        o = make()
+        same += memory(o).data_ptr() == at
+        if given:
+            got = call(o, stream=side)
+        else:
+            with torch.cuda.stream(side):
+                got = call(o)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        held.append(o)
+    assert same > 0                                                   # (else nothing was tried)
+
+
+@pytest.mark.parametrize("name", ["attention", "linear"])
+@pytest.mark.parametrize("given", [True, False])
+def test_objects_that_go_while_another_stream_uses_them(name, given):
+    """Their memory is not handed out before that stream is done."""
+    make, call, memory = attention_and_linear()[name]
+    side = torch.cuda.Stream()
+    want = call(make()).clone()
+    out = torch.empty_like(want)
+    o = make()
+    torch.cuda.synchronize()
+    n, at = memory(o).numel(), memory(o).data_ptr()
+    with torch.cuda.stream(side):
+        busy(1 << 20)
+        if not given:
+            call(o, out=out)
+    if given:
+        call(o, out=out, stream=side)
+    del o
+    new = torch.zeros(n, dtype=torch.uint8, device="cuda")
+    apart = new.data_ptr() >= at + n or at >= new.data_ptr() + n
+    torch.cuda.synchronize()
+    assert apart and torch.equal(out, want)
+
+
 def test_binding_refuses_wrong_tensors():
     x = torch.randn(4, 2, 64, device="cuda")
     pos = torch.zeros(4, dtype=I32, device="cuda")

@@ -172,6 +172,21 @@ def test_binding_refuses_a_stream_of_another_device():
         sm._raw_stream(torch.device("cuda", 0), Stream)
 
 
+class Stream:
+    """A stream by its number, with what is asked of it."""
+    device = torch.device("cuda", 0)
+
+    def __init__(self, number):
+        self.cuda_stream, self.log = number, []
+
+    def record_event(self):
+        self.log.append("recorded")
+        return "event of %d" % self.cuda_stream
+
+    def wait_event(self, event):
+        self.log.append(event)
+
+
 def without_gpu(monkeypatch, **calls):
     """The binding with host tensors and Python functions in the library's place."""
     class Lib:
@@ -181,6 +196,9 @@ def without_gpu(monkeypatch, **calls):
     monkeypatch.setattr(sm, "lib", lambda: Lib)
     monkeypatch.setattr(sm, "_device", lambda: torch.device("cpu"))
     monkeypatch.setattr(sm, "_raw_stream", lambda device, stream: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(0))
+    monkeypatch.setattr(sm, "_capturing", lambda stream: False)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: None)
     empty = torch.empty
     monkeypatch.setattr(torch, "empty", lambda *a, **kw: empty(*a, **{**kw, "device": "cpu"}))
 
@@ -254,3 +272,47 @@ def test_paged_attention_from_two_threads_one_call_at_a_time(monkeypatch):
     without_gpu(monkeypatch, sm_paged_attention=call)
     in_threads(*paged_attention_calls(sm.PagedAttention(4, 8, 2, 64, 16, 8, 6, torch.float32)), n=1000)
     assert max(met) == 1
+
+
+def test_memory_of_an_object_on_streams_other_than_its_own(monkeypatch):
+    """The first call on each stream waits for what the memory was made from, and keeps it from being handed out early; a captured stream cannot wait
+    for what is not in its graph, so its first call outside does."""
+    class Memory:
+        def __init__(self):
+            self.streams = []
+
+        def record_stream(self, s):
+            self.streams.append(s.cuda_stream)
+
+    dev, capturing = torch.device("cuda", 0), []
+    made, side, third = Stream(5), Stream(6), Stream(7)
+    monkeypatch.setattr(sm, "_capturing", lambda s: s.cuda_stream in capturing)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: side)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: side.cuda_stream, raising=False)
+    ws, bias = Memory(), Memory()
+    kept = sm._Kept(dev, made, ws, bias)
+    assert made.log == ["recorded"] and ws.streams == bias.streams == [5]
+    assert kept.used_on(dev, made) == 5 and made.log == ["recorded"]
+    for _ in range(3):                                               # the current stream, first
+        assert kept.used_on(dev, None) == 6
+        assert side.log == ["event of 5"] and ws.streams == bias.streams == [5, 6]
+    capturing.append(7)
+    assert kept.used_on(dev, third) == 7 and third.log == [] and ws.streams == [5, 6, 7]
+    capturing.clear()
+    assert kept.used_on(dev, third) == 7 and kept.used_on(dev, third) == 7 and third.log == ["event of 5"]
+    capturing.append(6)                                              # made while a graph is captured: nothing to wait for outside it
+    kept = sm._Kept(dev, None, ws)
+    assert kept.used_on(dev, made) == 5 and made.log == ["recorded"]
+
+
+def test_objects_use_their_memory_through_its_streams(monkeypatch):
+    got = []
+    without_gpu(monkeypatch, sm_paged_attention=lambda *a: got.append(a[-1]) or 0, sm_linear_w4=lambda *a: got.append(a[-1]) or 0, sm_linear_w4_pack=lambda *a: 0,
+                sm_linear_w4_packed_bytes=lambda *a: 64)
+    monkeypatch.setattr(sm._Kept, "used_on", lambda self, device, stream: tuple(t.data_ptr() for t in self.tensors))
+    att = sm.PagedAttention(4, 8, 2, 64, 16, 8, 6, torch.float32)
+    paged_attention_calls(att)[0]()
+    bias = torch.zeros(8, dtype=torch.bfloat16)
+    lin = sm.LinearW4(torch.zeros(8, 16, dtype=torch.uint8), torch.zeros(8, 1, dtype=torch.bfloat16), group=32, bias=bias)
+    lin(torch.zeros(2, 32, dtype=torch.bfloat16))
+    assert got == [(att.ws.data_ptr(),), (lin.packed.data_ptr(), bias.data_ptr())]
