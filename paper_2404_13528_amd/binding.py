@@ -859,6 +859,14 @@ def _new(shape, dtype, device, stream):
     return t
 
 
+def _lend(stream, *tensors):
+    """The caller's tensors, about to be used on a stream that was given: if the caller lets them go, they are not handed out before it is done."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
 class _Kept:
     """Device memory that an object keeps from call to call.  It is made on one stream, where work on what lay there before may be pending and a kernel
     may be filling it, and used on any: a stream's first call waits for that, and if the object goes, the memory is not handed out again
@@ -1073,6 +1081,7 @@ class LinearW4:
             _flat(bias, "bias", torch.bfloat16, (N,), dev)
         self.N, self.K, self.group, self.bias = N, 2 * half, group, bias
         self.packed = _new(n, u8, dev, stream)
+        _lend(stream, w, scales, zeros)
         check(lib().sm_linear_w4_pack(wp, sp, zp, N, self.K, group, self.packed.data_ptr(), _raw_stream(dev, stream)), "sm_linear_w4_pack")
         self._kept = _Kept(dev, stream, self.packed, *(() if bias is None else (bias,)))
 

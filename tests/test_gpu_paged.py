@@ -785,6 +785,28 @@ def test_objects_that_go_while_another_stream_uses_them(name, given):
     assert apart and torch.equal(out, want)
 
 
+def test_weights_dropped_while_another_stream_packs_them():
+    """LinearW4 on a stream that is busy: the sources go at once, and tensors of their size are filled on the current stream."""
+    g = torch.Generator().manual_seed(18)
+    w, sc = torch.randint(0, 256, (4096, 1024), generator=g, dtype=torch.uint8).cuda(), torch.rand(4096, 16, generator=g).to(BF16).cuda()
+    z = torch.randint(0, 16, (4096, 16), generator=g, dtype=torch.uint8).cuda()
+    want = sm.LinearW4(w, sc, z).packed.clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        a = [t.clone() for t in (w, sc, z)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            busy(1 << 20)
+        lin = sm.LinearW4(*a, stream=side)
+        at = {t.data_ptr() for t in a}
+        del a
+        new = [torch.zeros_like(t) for t in (w, sc, z)]
+        apart = not at & {t.data_ptr() for t in new}
+        torch.cuda.synchronize()
+        assert apart and torch.equal(lin.packed, want)
+
+
 def test_binding_refuses_wrong_tensors():
     x = torch.randn(4, 2, 64, device="cuda")
     pos = torch.zeros(4, dtype=I32, device="cuda")

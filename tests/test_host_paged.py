@@ -1,5 +1,6 @@
 """Host side of the paged-cache operators and the 4-bit Linear without a GPU: what is refused, and that it is refused before any
 pointer is looked at (the pointers here are made up)."""
+import contextlib
 import ctypes as C
 import sys
 import threading
@@ -316,3 +317,22 @@ def test_objects_use_their_memory_through_its_streams(monkeypatch):
     lin = sm.LinearW4(torch.zeros(8, 16, dtype=torch.uint8), torch.zeros(8, 1, dtype=torch.bfloat16), group=32, bias=bias)
     lin(torch.zeros(2, 32, dtype=torch.bfloat16))
     assert got == [(att.ws.data_ptr(),), (lin.packed.data_ptr(), bias.data_ptr())]
+
+
+def recorded(monkeypatch):
+    """What record_stream is told from now on: (address, stream)."""
+    seen = set()
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: seen.add((t.data_ptr(), s.cuda_stream)))
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    return seen
+
+
+def test_weights_stay_allocated_until_they_are_packed(monkeypatch):
+    without_gpu(monkeypatch, sm_linear_w4_pack=lambda *a: 0, sm_linear_w4_packed_bytes=lambda *a: 64)
+    seen = recorded(monkeypatch)
+    w, scales, zeros = torch.zeros(8, 16, dtype=torch.uint8), torch.zeros(8, 1, dtype=torch.bfloat16), torch.zeros(8, 1, dtype=torch.uint8)
+    sm.LinearW4(w, scales, zeros, group=32, stream=Stream(9))
+    assert {(t.data_ptr(), 9) for t in (w, scales, zeros)} <= seen
+    seen.clear()
+    sm.LinearW4(w, scales, group=32, stream=Stream(9))
+    assert {(t.data_ptr(), 9) for t in (w, scales)} <= seen
