@@ -860,11 +860,11 @@ def _new(shape, dtype, device, stream):
 
 
 def _lend(stream, *tensors):
-    """The caller's tensors, about to be used on a stream that was given: if the caller lets them go, they are not handed out before it is done."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+    """The caller's tensors (None: not there), about to be used on a stream that was given: if the caller lets them go, they are not handed out
+    before it is done."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
 
 
 class _Kept:
@@ -936,7 +936,10 @@ def page_table(cached, fresh, free_pages, n_free, table, page, n_pages, max_toke
         ptrs = (at, lens, pos, pos + 4 * n, pos + 8 * n)
     else:
         ptrs = [_flat(t, name, i32, (k,), dev) for t, name, k in zip(out, PageTable._fields, sizes)]
-    check(lib().sm_page_table(cfg, *ins, *ptrs, _raw_stream(dev, stream)), "sm_page_table")
+    raw = _raw_stream(dev, stream)
+    if stream is not None:
+        _lend(stream, cached, fresh, free_pages, n_free, table, *(out or ()))
+    check(lib().sm_page_table(cfg, *ins, *ptrs, raw), "sm_page_table")
     return PageTable(*whole.split_with_sizes(sizes)) if out is None else out
 
 
@@ -1003,7 +1006,10 @@ def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gam
                                 0 if q_beta is None else _flat(q_beta, "q_beta", dt, vec, dev), 0 if k_gamma is None else _flat(k_gamma, "k_gamma", dt, vec, dev),
                                 0 if k_beta is None else _flat(k_beta, "k_beta", dt, vec, dev), d if rot is None else rot, rope_base, page, n_pages,
                                 *qs, *ks, *vs, *qos, *kos, *vos)
-    check(lib().sm_head_norm_rope(desc, qp, kp, vp, _flat(positions, "positions", i32, (T,), dev), at, qo, ko, vo, _raw_stream(dev, stream)), "sm_head_norm_rope")
+    pos, raw = _flat(positions, "positions", i32, (T,), dev), _raw_stream(dev, stream)
+    if stream is not None:
+        _lend(stream, q, k, v, positions, slots, q_gamma, k_gamma, q_beta, k_beta, q_out, k_out, v_out)
+    check(lib().sm_head_norm_rope(desc, qp, kp, vp, pos, at, qo, ko, vo, raw), "sm_head_norm_rope")
     return (None if q is None else q_out), (None if k is None else k_out), (None if v is None else v_out)
 
 
@@ -1050,6 +1056,8 @@ class PagedAttention:
         desc = _PAGED_ATTENTION.pack(*self.sizes, table.stride(0) if self.table_shape[0] > 1 else self.table_shape[1], *q.stride()[:2], *out.stride()[:2],
                                      *k_pages.stride()[:3], *v_pages.stride()[:3])
         raw = self._kept.used_on(dev, stream)
+        if stream is not None:
+            _lend(stream, q, k_pages, v_pages, table, lens, out, lse)
         with self._one:                           # (a call's two kernels follow each other in the stream)
             check(lib().sm_paged_attention(desc, *args, self.ws.numel(), raw), "sm_paged_attention")
         return out
@@ -1081,7 +1089,8 @@ class LinearW4:
             _flat(bias, "bias", torch.bfloat16, (N,), dev)
         self.N, self.K, self.group, self.bias = N, 2 * half, group, bias
         self.packed = _new(n, u8, dev, stream)
-        _lend(stream, w, scales, zeros)
+        if stream is not None:
+            _lend(stream, w, scales, zeros)
         check(lib().sm_linear_w4_pack(wp, sp, zp, N, self.K, group, self.packed.data_ptr(), _raw_stream(dev, stream)), "sm_linear_w4_pack")
         self._kept = _Kept(dev, stream, self.packed, *(() if bias is None else (bias,)))
 
@@ -1095,9 +1104,12 @@ class LinearW4:
             op = out.data_ptr()
         else:
             op = _flat(out, "out", bf16, shape, dev)
-        check(lib().sm_linear_w4(_LINEAR_W4.pack(M, self.N, self.K, self.group, ACT[act]), xp, _flat(self.packed, "the packed weights", torch.uint8, self.packed.shape, dev),
-                                 None if self.bias is None else self.bias.data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev),
-                                 op, self._kept.used_on(dev, stream)), "sm_linear_w4")
+        args = (_LINEAR_W4.pack(M, self.N, self.K, self.group, ACT[act]), xp, _flat(self.packed, "the packed weights", torch.uint8, self.packed.shape, dev),
+                None if self.bias is None else self.bias.data_ptr(), None if residual is None else _flat(residual, "residual", bf16, shape, dev), op)
+        raw = self._kept.used_on(dev, stream)
+        if stream is not None:
+            _lend(stream, x, residual, out)
+        check(lib().sm_linear_w4(*args, raw), "sm_linear_w4")
         return out
 
 

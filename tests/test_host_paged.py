@@ -336,3 +336,31 @@ def test_weights_stay_allocated_until_they_are_packed(monkeypatch):
     seen.clear()
     sm.LinearW4(w, scales, group=32, stream=Stream(9))
     assert {(t.data_ptr(), 9) for t in (w, scales)} <= seen
+
+
+def test_tensors_of_a_call_stay_allocated_until_its_stream_is_done(monkeypatch):
+    without_gpu(monkeypatch, sm_paged_attention=lambda *a: 0, sm_linear_w4=lambda *a: 0, sm_linear_w4_pack=lambda *a: 0, sm_linear_w4_packed_bytes=lambda *a: 64,
+                sm_page_table=lambda *a: 0, sm_head_norm_rope=lambda *a: 0)
+    i32, bf16 = torch.int32, torch.bfloat16
+    att = sm.PagedAttention(4, 8, 2, 64, 16, 8, 6, torch.float32)
+    lin = sm.LinearW4(torch.zeros(8, 16, dtype=torch.uint8), torch.zeros(8, 1, dtype=bf16), group=32)
+    q, kp, vp, out, lse = torch.zeros(4, 8, 64), torch.zeros(6, 16, 2, 64), torch.zeros(6, 16, 2, 64), torch.zeros(4, 8, 64), torch.zeros(4, 8)
+    table, lens = torch.zeros(4, 8, dtype=i32), torch.zeros(4, dtype=i32)
+    k, v, gains, pos, slots = torch.zeros(4, 2, 64), torch.zeros(4, 2, 64), torch.zeros(4, 64), torch.zeros(4, dtype=i32), torch.zeros(4, dtype=i32)
+    x, res, y = torch.zeros(2, 32, dtype=bf16), torch.zeros(2, 8, dtype=bf16), torch.zeros(2, 8, dtype=bf16)
+    cached, fresh, free, n_free = (torch.zeros(n, dtype=i32) for n in (4, 4, 6, 1))
+    pt = sm.PageTable(*(torch.zeros(n, dtype=i32) for n in (5, 4, 3, 3, 1)))
+    calls = [(lambda s: att(q, kp, vp, table, lens, out=out, lse=lse, stream=s), (q, kp, vp, table, lens, out, lse)),
+             (lambda s: lin(x, residual=res, out=y, stream=s), (x, res, y)),
+             (lambda s: sm.page_table(cached, fresh, free, n_free, table, 16, 6, 3, out=pt, stream=s), (cached, fresh, free, n_free, table, *pt)),
+             (lambda s: sm.head_norm_rope(q, k, v, pos, "layer", q_gamma=gains[0], k_gamma=gains[1], q_beta=gains[2], k_beta=gains[3], slots=slots, q_out=out,
+                                          k_out=kp, v_out=vp, stream=s), (q, k, v, pos, *gains, slots, out, kp, vp)),
+             (lambda s: sm.head_norm_rope(None, None, v, pos, slots=slots, v_out=vp, stream=s), (v, pos, slots, vp))]
+    seen = recorded(monkeypatch)
+    for call, tensors in calls:
+        seen.clear()
+        call(Stream(9))
+        assert {(t.data_ptr(), 9) for t in tensors} <= seen
+    monkeypatch.setattr(torch.Tensor, "record_stream", None)         # the current stream: nothing to tell
+    for call, _ in calls:
+        call(None)
