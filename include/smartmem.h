@@ -459,7 +459,7 @@ int sm_decode_step(const sm_decode_cfg*, const sm_decode_weights*, const void* x
  *     be had because free_pages ran out, and where the page id lies outside [0, n_pages)
  *   lens [n_req]: tokens that the request's pages hold after the iteration: c + fresh[r], less what found no row or page
  *   need [1]: pages the call wanted; free_pages ran out if it exceeds *n_free.  The first min(*need, *n_free) are taken.
- * The outputs must not overlap the inputs (except `table`, which is both).  The same call again gives the same result.
+ * Outputs that overlap an input or each other are refused (`table` is both).  The same call again gives the same result.
  * Limits: n_req <= 65536, max_tokens, n_req * max_pages, n_pages * page and max_pages * page <= 2^30. */
 typedef struct { int32_t n_req, page, max_pages, n_pages, free_cap, max_tokens; int64_t table_pitch; } sm_page_cfg;
 int sm_page_table(const sm_page_cfg*, const int32_t* cached, const int32_t* fresh, const int32_t* free_pages, const int32_t* n_free,

@@ -1,4 +1,5 @@
 // C ABI of the operators over a paged key / value cache and of the 4-bit Linear: validation, then the launches.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include "common.h"
@@ -17,6 +18,16 @@ int64_t pool_units(const int64_t (&s)[3], int n_pages, int page, int vec) {
   const int64_t v = (int64_t)(page - 1) * (s[1] / vec);
   return u < top && v < top && u + v < top ? u + v : -1;
 }
+// An array of `rows` rows of `width` bytes, `pitch` >= width apart; a plain array is one row.
+struct Span { const void* p; uint64_t width, rows, pitch; };
+// whether a plain array and another have a byte in common
+bool meet(const Span& plain, const Span& s) {
+  const uint64_t lo = reinterpret_cast<uintptr_t>(plain.p), hi = lo + plain.width, at = reinterpret_cast<uintptr_t>(s.p);
+  if (!plain.width || !s.width) return false;
+  const uint64_t k = lo <= at || s.rows == 1 ? 0 : std::min((lo - at) / s.pitch, s.rows - 1);      // the last row that starts at or before lo, or the first
+  return (lo < at + k * s.pitch + s.width && hi > at + k * s.pitch) || (k + 1 < s.rows && hi > at + (k + 1) * s.pitch);
+}
+Span flat(const void* p, uint64_t bytes) { return Span{p, p ? bytes : 0, 1, 0}; }
 template <int N> bool multiples(const int64_t (&s)[N], int vec) {
   for (int64_t v : s) if (v % vec) return false;
   return true;
@@ -36,6 +47,13 @@ extern "C" int sm_page_table(const sm_page_cfg* c, const int32_t* cached, const 
     return fail(SM_ERR_INVALID_ARG, "%s: null pointer", who);
   const void* all[11] = {cached, fresh, free_pages, n_free, table, starts, lens, positions, slots, need, nullptr};
   for (const void* p : all) if (!aligned4(p)) return fail(SM_ERR_INVALID_ARG, "%s: arrays must be 4-byte aligned", who);
+  const uint64_t R = (uint64_t)c->n_req, T = (uint64_t)c->max_tokens;
+  const Span spans[10] = {flat(starts, 4 * (R + 1)), flat(lens, 4 * R), flat(positions, 4 * T), flat(slots, 4 * T), flat(need, 4),      // written
+                          flat(cached, 4 * R), flat(fresh, 4 * R), flat(free_pages, 4 * (uint64_t)c->free_cap), flat(n_free, 4),
+                          Span{table, 4 * (uint64_t)c->max_pages, R, 4 * (uint64_t)c->table_pitch}};
+  for (int i = 0; i < 9; ++i)
+    for (int j = i + 1; j < 10; ++j)
+      if ((i < 5 || j == 9) && meet(spans[i], spans[j])) return fail(SM_ERR_INVALID_ARG, "%s: an output overlaps an input or another output", who);
   PageTableArgs a{cached, fresh, free_pages, n_free, table, starts, lens, positions, slots, need,
                   c->n_req, c->page, c->max_pages, c->n_pages, c->free_cap, c->max_tokens, c->table_pitch};
   char label[96] = "";

@@ -102,6 +102,32 @@ def test_page_table_bad_pages_have_no_slot():
     assert out.slots.tolist() == [-1, -1, -1, -1] and out.lens.tolist() == [2, 2, 2]
 
 
+def test_page_table_with_its_arrays_side_by_side_and_between_the_rows_of_the_table():
+    """Everything in one buffer, adjacent or in the gap of the table's pitch: nothing overlaps, nothing is refused."""
+    buf = torch.full((400,), -9, dtype=I32, device="cuda")
+    table = buf[:90].view(3, 30)[:, :4]
+    at = [90]
+
+    def piece(n, values=None):
+        t = buf[at[0]:at[0] + n]
+        at[0] += n
+        if values is not None:
+            t.copy_(ints(values))
+        return t
+    cached, fresh = piece(3, [5, 0, 9]), piece(3, [2, 3, 9])
+    free, n_free = buf[34:44], buf[74:75]                               # (rows 1 and 2 of the table begin at 30 and 60)
+    free.copy_(torch.arange(50, 60, dtype=I32))
+    n_free.fill_(10)
+    table.copy_(ints([[7, -1, -1, -1], [-1] * 4, [3, 2, -1, -1]]))
+    out = sm.PageTable(piece(4), piece(3), piece(15), piece(15), buf[89:90])
+    want = P.page_table([5, 0, 9], [2, 3, 9], list(range(50, 60)), 10, table.cpu().numpy(), 8, 64, 15)
+    sm.page_table(cached, fresh, free, n_free, table, 8, 64, 15, out=out)
+    assert (table.cpu().numpy() == want[0]).all() and all((g.cpu().numpy() == w).all() for g, w in zip(out, want[1:]))
+    assert (buf[at[0]:] == -9).all() and (buf[4:30] == -9).all()
+    with pytest.raises(sm.SmError, match="overlap"):
+        sm.page_table(out.lens, fresh, free, n_free, table, 8, 64, 15, out=out)      # (the next iteration needs other outputs)
+
+
 def test_page_table_counts_at_the_limits():
     """Lengths and capacities at 2^30, where sums of two of them do not fit 31 bits."""
     big = 2 ** 30

@@ -364,3 +364,17 @@ def test_tensors_of_a_call_stay_allocated_until_its_stream_is_done(monkeypatch):
     monkeypatch.setattr(torch.Tensor, "record_stream", None)         # the current stream: nothing to tell
     for call, _ in calls:
         call(None)
+
+
+def test_page_table_refuses_outputs_over_inputs_or_each_other():
+    """cached, fresh, free_pages (32), n_free, table (4 rows of 8, 24 apart), starts (5), lens, positions (10), slots (10), need."""
+    sizes = [4, 4, 32, 1, 3 * 24 + 8, 5, 4, 10, 10, 1]
+    base = [(1 << 20) + (1 << 12) * i for i in range(10)]
+    cfg = page_cfg(table_pitch=24)
+    for i in range(4, 10):
+        for j in range(10):
+            if i == j:
+                continue
+            for at in (base[j], base[j] + 4 * (sizes[j] - 1), base[j] - 4 * (sizes[i] - 1)):         # first, last and first place in common
+                p = [C.c_void_p(at if k == i else base[k]) for k in range(10)]
+                assert page_call(cfg, *p) == -1 and b"overlap" in sm.lib().sm_last_error(), (i, j, at)
