@@ -514,7 +514,7 @@ int sm_paged_attention(const sm_paged_attention_desc*, const void* q, const void
  * SM_ACT_NONE or SM_ACT_GELU (erf).  sm_linear_w4_pack writes weights, scales and zero points into `packed`
  * (sm_linear_w4_packed_bytes, caller-owned device memory) in the order the kernel reads them, once.  The products are
  * exact (integers times bf16, fp32 sums); a group's sum takes its scale in fp32; a row of x with an infinity or a NaN gives
- * NaN.  y may be the residual, but must not overlap x.  Made for the rows of a decode step: the weights are streamed once
+ * NaN.  y may be the residual; any other overlap with an operand is refused.  Made for the rows of a decode step: the weights are streamed once
  * per 32 rows at best. */
 typedef struct { int32_t M, N, K, group, act; } sm_linear_w4_desc;
 size_t sm_linear_w4_packed_bytes(int N, int K, int group);

@@ -178,6 +178,10 @@ extern "C" int sm_linear_w4_pack(const void* w, const void* scales, const void* 
   if (int rc = check_w4(N, K, group, who)) return rc;
   if (!w || !scales || !packed) return fail(SM_ERR_INVALID_ARG, "%s: null pointer", who);
   if (!aligned16(w) || !aligned16(scales) || !aligned16(packed)) return fail(SM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  const Span out = flat(packed, w4_packed_bytes(N, K, group));
+  const uint64_t groups = (uint64_t)N * (K / group);
+  for (const Span& in : {flat(w, (uint64_t)N * K / 2), flat(scales, 2 * groups), flat(zeros, groups)})
+    if (meet(out, in)) return fail(SM_ERR_INVALID_ARG, "%s: the packed weights overlap their sources", who);
   Timed tm("linear_w4_pack", stream);
   if (int e = launch_w4_pack(w, scales, zeros, N, K, group, packed, stream)) return fail(SM_ERR_DEVICE, "%s: launch failed (hip error %d)", who, e);
   return SM_OK;
@@ -192,6 +196,10 @@ extern "C" int sm_linear_w4(const sm_linear_w4_desc* c, const void* x, const voi
   if (c->M == 0) return SM_OK;                       // no rows: nothing is launched
   if (!x || !packed || !y) return fail(SM_ERR_INVALID_ARG, "%s: null pointer", who);
   if (!aligned16(x) || !aligned16(packed) || !aligned16(y) || !aligned16(bias) || !aligned16(residual)) return fail(SM_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", who);
+  const Span out = flat(y, 2 * (uint64_t)c->M * c->N);
+  for (const Span& in : {flat(x, 2 * (uint64_t)c->M * c->K), flat(packed, w4_packed_bytes(c->N, c->K, c->group)), flat(bias, 2 * (uint64_t)c->N),
+                         flat(y == residual ? nullptr : residual, out.width)})
+    if (meet(out, in)) return fail(SM_ERR_INVALID_ARG, "%s: y overlaps an operand (it may be the residual)", who);
   LinearW4Args a{x, packed, bias, residual, y, c->M, c->N, c->K, c->group, c->act};
   char label[96] = "";
   if (timing_on()) snprintf(label, sizeof(label), "linear_w4g%d[%d,%d,%d]%s%s", c->group, c->M, c->N, c->K, c->act ? "+gelu" : "", residual ? "+res" : "");

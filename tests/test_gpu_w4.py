@@ -93,6 +93,17 @@ def test_rows_do_not_touch_each_other():
     assert lin(x[:0]).shape == (0, 70)
 
 
+def test_results_over_operands_are_refused():
+    lin = sm.LinearW4(torch.zeros(128, 64, dtype=torch.uint8, device="cuda"), torch.ones(128, 1, dtype=BF16, device="cuda"), group=128)
+    buf = torch.ones(64, 128, dtype=BF16, device="cuda")
+    with pytest.raises(sm.SmError, match="overlap"):
+        lin(buf[:8], out=buf[:8])
+    with pytest.raises(sm.SmError, match="overlap"):
+        lin(buf[:8], residual=buf[16:24], out=buf[17:25])
+    # 128 weights of -8, and 1: -1023, in bf16 -1024
+    assert (lin(buf[:8], residual=buf[8:16], out=buf[16:24]) == -1024).all() and (buf[:16] == 1).all() and (buf[24:] == 1).all()
+
+
 def test_captured_and_replayed():
     g = torch.Generator().manual_seed(4)
     lin = sm.LinearW4(torch.randint(0, 256, (512, 512), generator=g, dtype=torch.uint8).cuda(), torch.rand(512, 8, generator=g).to(BF16).cuda(), group=128)

@@ -378,3 +378,16 @@ def test_page_table_refuses_outputs_over_inputs_or_each_other():
             for at in (base[j], base[j] + 4 * (sizes[j] - 1), base[j] - 4 * (sizes[i] - 1)):         # first, last and first place in common
                 p = [C.c_void_p(at if k == i else base[k]) for k in range(10)]
                 assert page_call(cfg, *p) == -1 and b"overlap" in sm.lib().sm_last_error(), (i, j, at)
+
+
+def test_w4_refuses_results_over_operands():
+    lib, d = sm.lib(), sm.LinearW4Desc(4, 64, 128, 128, 0)
+    x, packed, bias, residual, y = ((1 << 20) + (1 << 16) * i for i in range(5))
+    nbytes = {x: 4 * 128 * 2, packed: lib.sm_linear_w4_packed_bytes(64, 128, 128), bias: 128, residual: 512}
+    for p, n in nbytes.items():
+        for at in (p, p + n - 16, p - 512 + 16):
+            if at != residual:
+                assert lib.sm_linear_w4(C.byref(d), x, packed, bias, residual, at, None) == -1 and b"overlap" in lib.sm_last_error(), (p, at)
+    for p, n in ((x, 64 * 64), (bias, 128), (residual, 64)):                                          # weights, scales, zero points
+        for at in (p, p + n - 16, p - nbytes[packed] + 16):
+            assert lib.sm_linear_w4_pack(x, bias, residual, 64, 128, 128, at, None) == -1 and b"overlap" in lib.sm_last_error()
