@@ -76,6 +76,7 @@ extern "C" int sm_head_norm_rope(const sm_head_norm_rope_desc* c, const void* q,
   if (c->rot < 0 || c->rot > c->d || c->rot % (2 * vec)) return fail(SM_ERR_SHAPE, "%s: rotated features must be a multiple of %d, at most the head size", who, 2 * vec);
   if (c->norm < 0 || c->norm > 2) return fail(SM_ERR_INVALID_ARG, "%s: unknown norm %d", who, c->norm);
   if (c->rot && !(c->rope_base >= 1.f && std::isfinite(c->rope_base))) return fail(SM_ERR_INVALID_ARG, "%s: the rotation's base must be at least 1", who);
+  if (!k && !v) slots = nullptr;                     // (places of keys and values only)
   if (slots && (c->page < 1 || c->n_pages < 1 || (int64_t)c->page * c->n_pages > CAP)) return fail(SM_ERR_SHAPE, "%s: bad page pool", who);
   if (c->tokens == 0) return SM_OK;                  // no tokens: no pointer is looked at, nothing is launched
   if (!q && !k && !v) return fail(SM_ERR_INVALID_ARG, "%s: nothing to do: q, k and v are null", who);

@@ -261,6 +261,16 @@ def test_head_norm_rope_parts_in_place_and_empty():
     assert not o[0, 0].any() and not o[1, 1].any() and not o[0, 1].isfinite().all() and o[1, 0].isnan().all()
 
 
+@pytest.mark.parametrize("T", [6, 900])
+def test_head_norm_rope_queries_alone_beside_slots(T):
+    """Slots name places of keys and values; queries by themselves go to their rows whatever the slots say."""
+    g = torch.Generator().manual_seed(T)
+    q, gain, pos = torch.randn(T, 3, 64, generator=g).cuda(), torch.ones(64, device="cuda"), torch.arange(T, dtype=I32, device="cuda")
+    slots = torch.arange(T, dtype=I32, device="cuda") - 2
+    got = sm.head_norm_rope(q, None, None, pos, q_gamma=gain, slots=slots)
+    assert torch.equal(got[0], sm.head_norm_rope(q, None, None, pos, q_gamma=gain)[0]) and got[1] is None and got[2] is None
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("T", [5, 900])
 @pytest.mark.parametrize("d, rot", [(64, 32), (128, 32), (128, 96), (256, 64), (96, 0)])
