@@ -92,10 +92,10 @@ extern "C" int sm_head_norm_rope(const sm_head_norm_rope_desc* c, const void* q,
       (v && (!multiples(c->v_stride, vec) || !multiples(c->v_out_stride, vec))))
     return fail(SM_ERR_SHAPE, "%s: strides must keep 16-byte alignment", who);
   HeadNormArgs a; std::memset(&a, 0, sizeof(a));
-  if (q) a.part[0] = HeadNormPart{q, c->q_gamma, c->q_beta, q_out, c->q_stride[0], c->q_stride[1], 0, c->q_out_stride[0], c->q_out_stride[1], c->heads_q, 0, 1, 0};
+  if (q) a.part[0] = HeadNormPart{q, c->q_gamma, c->q_beta, q_out, c->q_stride[0], c->q_stride[1], 0, c->q_out_stride[0], c->q_out_stride[1], c->heads_q, 0, 0};
   const int paged = slots != nullptr;
-  if (k) a.part[1] = HeadNormPart{k, c->k_gamma, c->k_beta, k_out, c->k_stride[0], c->k_stride[1], c->k_out_stride[0], c->k_out_stride[1], c->k_out_stride[2], c->heads_kv, 0, 1, paged};
-  if (v) a.part[2] = HeadNormPart{v, nullptr, nullptr, v_out, c->v_stride[0], c->v_stride[1], c->v_out_stride[0], c->v_out_stride[1], c->v_out_stride[2], c->heads_kv, 0, 0, paged};
+  if (k) a.part[1] = HeadNormPart{k, c->k_gamma, c->k_beta, k_out, c->k_stride[0], c->k_stride[1], c->k_out_stride[0], c->k_out_stride[1], c->k_out_stride[2], c->heads_kv, 0, paged};
+  if (v) a.part[2] = HeadNormPart{v, nullptr, nullptr, v_out, c->v_stride[0], c->v_stride[1], c->v_out_stride[0], c->v_out_stride[1], c->v_out_stride[2], c->heads_kv, 0, paged};
   if (c->rot) {
     // theta_i / 2 pi in 64 bits behind the point.  The repeated product in 64-bit mantissas is off by at most 2 i 2^-64 of theta_i / 2 pi
     // <= 0.16, with at most 127 factors 2^-58: at positions below 2^31 less than 2^-27 of a revolution

@@ -18,7 +18,7 @@ constexpr int HN_MAX_PAIRS = 128;
 struct HeadNormPart {               // q, k or v: one input and where its rows go
   const void *x, *gamma, *beta; void* y;
   int64_t x_t, x_h, y_page, y_t, y_h;
-  int heads, units, rotate, paged;  // units: groups of heads that a wave takes at once; rotate 0: copied as it is
+  int heads, units, paged;          // units: groups of heads that a wave takes at once
 };
 struct HeadNormArgs {
   uint64_t turn[HN_MAX_PAIRS];      // theta_i / 2 pi as a fraction of 2^64
