@@ -571,6 +571,56 @@ def test_paged_attention_is_deterministic_and_free_of_its_neighbours():
         assert torch.equal(att(q, kp, vp, table, lens), a)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_paged_attention_of_a_request_beside_others(dtype):
+    """The other lengths of a batch decide how long a chunk is: alone (one unit), among empty and short requests, beside one of 60000 keys (two units)
+    and one of 400000 (the longest chunk).  The request's result stays the oracle's within the rounding of its sums."""
+    g = torch.Generator().manual_seed(19)
+    n, hq, hkv, d, page, n_pages = 1600, 4, 2, 64, 16, 150
+    kp, vp = torch.randn(2, n_pages, page, hkv, d, generator=g).to(dtype)
+    q1, row = torch.randn(1, hq, d, generator=g).to(dtype), torch.randperm(n_pages, generator=g)[:100]
+    o, lse, av, aw = P.paged_attention(to_np(q1), to_np(kp), to_np(vp), row[None].numpy(), [n], d ** -0.5, want_bound=True)
+    score = (d + 4) * 2.0 ** -24 * aw + (np.abs(lse)[..., None] + 4) * 2.0 ** -23
+    weight = 2.0 ** -22 + (n / 16 + 64) * 2.0 ** -24
+    kd, vd = kp.cuda(), vp.cuda()
+    for others in ([], [0, 1, 17, 0, 300, 5] * 5, [60000], [3, 400000], [-2 ** 31, 2 ** 31 - 1, 200]):
+        lens = others[:len(others) // 2] + [n] + others[len(others) // 2:]
+        r, R = len(others) // 2, len(lens)
+        cols = max(-(-min(max(x, 0), 10 ** 6) // page) for x in lens)              # (a length past the row ends at its end)
+        table = torch.randint(0, n_pages, (R, cols), generator=g)
+        table[r, :100] = row
+        q = torch.randn(R, hq, d, generator=g).to(dtype)
+        q[r] = q1[0]
+        got_lse = torch.empty(R, hq, device="cuda")
+        got = sm.PagedAttention(R, hq, hkv, d, page, cols, n_pages, dtype)(q.cuda(), kd, vd, table.to(I32).cuda(), ints(lens), lse=got_lse)
+        check(got[r:r + 1], o, HALF[dtype] * np.abs(o) + (2 * score + weight) * av, "o beside %s" % others)
+        check(got_lse[r:r + 1], lse, 2 * score[..., 0] + weight + 2.0 ** -22 * (1 + np.abs(lse)), "lse beside %s" % others)
+        for i, x in enumerate(lens):
+            assert (x > 0) == got_lse[i].isfinite().all().item() and (x > 0 or not got[i].any() and (got_lse[i] == -np.inf).all())
+
+
+def test_objects_made_while_a_graph_is_captured():
+    """Workspace and packed weights are the graph's; replays on other lengths, eager calls of other objects in between."""
+    g = torch.Generator().manual_seed(20)
+    kp, vp = torch.randn(2, 200, 16, 2, 64, generator=g).to(BF16).cuda()
+    q, table = torch.randn(2, 4, 64, generator=g).to(BF16).cuda(), torch.randperm(200, generator=g).to(I32).cuda().reshape(2, 100)
+    w, sc = torch.randint(0, 256, (48, 128), generator=g, dtype=torch.uint8).cuda(), torch.rand(48, 2, generator=g).to(BF16).cuda()
+    lens = ints([0, 0])
+    eager, lin = sm.PagedAttention(2, 4, 2, 64, 16, 100, 200, BF16), sm.LinearW4(w, sc)
+    torch.cuda.synchronize()
+    cg = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(cg):
+        a, b = sm.PagedAttention(2, 4, 2, 64, 16, 100, 200, BF16), sm.LinearW4(w, sc)
+        o = a(q, kp, vp, table, lens)
+        y = b(o.view(2, 256))
+    for now in ([1600, 3], [0, 700], [1600, 1600]):
+        lens.copy_(ints(now))
+        cg.replay()
+        torch.cuda.synchronize()
+        want = eager(q, kp, vp, table, lens)
+        assert torch.equal(o, want) and torch.equal(y, lin(want.view(2, 256)))
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def serve(E, hq, hkv, d, page, dtype, prompts, steps, graph=False):

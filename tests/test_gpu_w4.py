@@ -75,6 +75,21 @@ def test_random(M, N, K, group, zeros, bias, residual, act):
     case(M, N, K, group, zeros, bias, residual, act, seed=N)
 
 
+@pytest.mark.parametrize("M", [1, 9, 20])
+@pytest.mark.parametrize("residual", [False, True])
+def test_gelu_of_exact_sums(M, residual):
+    """The argument is exact (integers, one power of two as the scale), so the result may be off by the error function's 1.5e-7 of half the argument, a few
+    roundings of fp32 and the store's half step (a GELU that is 3e-4 off would fail at the smaller values)."""
+    g = torch.Generator().manual_seed(M)
+    w, x = torch.randint(0, 256, (300, 64), generator=g, dtype=torch.uint8), torch.randint(-4, 5, (M, 128), generator=g).to(BF16)
+    s, r = torch.full((300, 1), 2.0 ** -7).to(BF16), torch.randn(M, 300, generator=g).to(BF16)
+    arg = P.linear_w4(to_np(x), w.numpy(), to_np(s), None, 128)
+    want = P.linear_w4(to_np(x), w.numpy(), to_np(s), None, 128, None, to_np(r) if residual else None, "gelu")
+    got = to_np(sm.LinearW4(w.cuda(), s.cuda())(x.cuda(), residual=r.cuda() if residual else None, act="gelu"))
+    tol = 2.0 ** -8 * np.abs(want) + 0.5 * np.abs(arg) * (1.5e-7 + 2.0 ** -21) + 2.0 ** -23 * np.abs(want)
+    assert np.abs(arg).max() > 3 and (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+
+
 def test_rows_do_not_touch_each_other():
     """A row of infinities or NaN stays in its row, and nothing is written around the result."""
     g = torch.Generator().manual_seed(3)
