@@ -475,7 +475,7 @@ int sm_page_table(const sm_page_cfg*, const int32_t* cached, const int32_t* fres
  * pools and row t goes to page slots[t] / page, place slots[t] % page; a slot outside [0, n_pages * page) stores nothing.
  * A token with a negative position is padding: nothing is stored for it.  Two tokens of one slot: each head of the slot
  * holds either of them.  An output may be its input (same address and strides), otherwise they must not overlap.
- * Angles are exact to 2^-27 of a revolution at any position.  rot a multiple of twice the 16-byte vector (16 bf16, 8 f32),
+ * Angles are exact to 2^-25 of a revolution at any position.  rot a multiple of twice the 16-byte vector (16 bf16, 8 f32),
  * d a multiple of the vector, both at most 256; rope_base >= 1; n_pages * page <= 2^30, tokens <= 2^25. */
 typedef struct {
   int32_t dtype, tokens, heads_q, heads_kv, d;
@@ -493,12 +493,15 @@ int sm_head_norm_rope(const sm_head_norm_rope_desc*, const void* q, const void* 
  * multiple of heads_kv).  No token (lens[r] <= 0, or no page of them exists), or none with a logit above -inf: o = 0,
  * lse = -inf.  A NaN among the logits: NaN.  lse (nullable) [n_req, heads_q] fp32, contiguous: the natural logarithm of
  * the sum of exp(scale * q . k), with which results over disjoint parts of a cache can be joined.  What lies in a page
- * behind the request's last token is not used, whatever it is.  o must not overlap the inputs.  Strides: request, head
- * (q, o); page, token, head (k_pages, v_pages: token-major [page, token, head, d] and head-major [page, head, token, d]
- * pools alike; page and token strides not negative, a pool's pages within 64 GiB).  The key axis is split over
- * workgroups by the lengths found on the device and joined in fp32.
+ * behind the request's last token is not used, whatever it is; finite values are taken at any size, and one of a key that
+ * weighs nothing adds nothing.  o must not overlap the inputs.  Strides: request, head (q, o); page, token, head (k_pages,
+ * v_pages: token-major [page, token, head, d] and head-major [page, head, token, d] pools alike; page and token strides not
+ * negative, a pool's pages within 64 GiB).  The key axis is split over workgroups by the lengths found on the device and
+ * joined in fp32.
  * d a multiple of the 16-byte vector (8 bf16, 4 f32), at most 256.  The workspace holds partial results; nothing in it
- * has to survive between calls; calls that share one on different streams race. */
+ * has to survive between calls; calls that share one on different streams race, and a call's two kernels have to follow
+ * each other in the stream: threads that share one call in turn.  Every workgroup reads all n_req lengths, so the time for
+ * them grows with the square of n_req: from some 500 short requests on, several calls are faster than one. */
 typedef struct {
   int32_t dtype, n_req, heads_q, heads_kv, d, page, max_pages, n_pages;
   float scale;
@@ -514,8 +517,8 @@ int sm_paged_attention(const sm_paged_attention_desc*, const void* q, const void
  * SM_ACT_NONE or SM_ACT_GELU (erf).  sm_linear_w4_pack writes weights, scales and zero points into `packed`
  * (sm_linear_w4_packed_bytes, caller-owned device memory) in the order the kernel reads them, once.  The products are
  * exact (integers times bf16, fp32 sums); a group's sum takes its scale in fp32; a row of x with an infinity or a NaN gives
- * NaN.  y may be the residual; any other overlap with an operand is refused.  Made for the rows of a decode step: the weights are streamed once
- * per 32 rows at best. */
+ * NaN, one with values from 2^113 on may.  All addresses are 16-byte aligned.  y may be the residual; any other overlap of it
+ * with an operand is refused.  Made for the rows of a decode step: the weights are streamed once per 32 rows at best. */
 typedef struct { int32_t M, N, K, group, act; } sm_linear_w4_desc;
 size_t sm_linear_w4_packed_bytes(int N, int K, int group);
 int sm_linear_w4_pack(const void* w, const void* scales, const void* zeros, int N, int K, int group, void* packed, void* stream);

@@ -784,7 +784,9 @@ class DecodeStep:
 # --------------------------------------------------------------------------
 
 # (A decode iteration makes these calls once per layer and they run for a few microseconds: what is right is found right by a few
-# comparisons, plain integers go to the library, and only a call that is refused pays for saying why.)
+# comparisons, plain integers go to the library, and only a call that is refused pays for saying why.
+# A call on a given stream finds its inputs there: if another stream fills them, the caller makes the given one wait.  The call's tensors then
+# stay allocated until the given stream is done with them, and results that the call makes are that stream's.)
 
 def _refuse(t, name, dtype, shape, device, rows):
     import torch
@@ -918,7 +920,8 @@ PageTable = collections.namedtuple("PageTable", "starts lens positions slots nee
 def page_table(cached, fresh, free_pages, n_free, table, page, n_pages, max_tokens, out=None, stream=None):
     """sm_page_table: pages and slots of the new tokens of an iteration, from lengths on the device.  cached, fresh [R], free_pages,
     n_free [1] and table [R, max_pages] (updated in place) are int32 device tensors.  Returns PageTable(starts [R + 1], lens [R],
-    positions [max_tokens], slots [max_tokens], need [1]) (parts of one new tensor), or fills the one given as `out`."""
+    positions [max_tokens], slots [max_tokens], need [1]) (parts of one new tensor), or fills the one given as `out`, which
+    must not overlap the inputs: the next iteration's `cached` may be this one's lens, but not its `out` as well."""
     import torch
     i32, dev = torch.int32, _device()
     R, cols = _dims(table, "table", 2)
@@ -957,9 +960,10 @@ HEAD_NORM = {"none": 0, "layer": 1, "rms": 2}
 def head_norm_rope(q, k, v, positions, norm="rms", eps=1e-5, q_gamma=None, k_gamma=None, q_beta=None, k_beta=None, rot=None,
                    rope_base=10000.0, slots=None, q_out=None, k_out=None, v_out=None, stream=None):
     """sm_head_norm_rope.  q [T, heads_q, d], k and v [T, heads_kv, d] (strided views; each may be None), positions [T] int32 (negative:
-    padding).  norm "rms" / "layer" / "none" over d; rot: rotated features (None: all d).  slots [T] int32: k and v go to their slots
-    of the pools k_out / v_out [n_pages, page, heads_kv, d] (strided views, so a head-major pool is passed permuted); without slots
-    k_out / v_out are [T, heads_kv, d] (new tensors by default), as q_out always is.  Returns (q_out, k_out, v_out)."""
+    padding, whose rows of the results stay as they were: anything, in new ones).  norm "rms" / "layer" / "none" over d; rot: rotated
+    features (None: all d).  slots [T] int32: k and v go to their slots of the pools k_out / v_out [n_pages, page, heads_kv, d] (strided
+    views, so a head-major pool is passed permuted); without slots k_out / v_out are [T, heads_kv, d] (new tensors by default), as
+    q_out always is.  Returns (q_out, k_out, v_out)."""
     import torch
     first = q if q is not None else k if k is not None else v
     if first is None:
@@ -1073,7 +1077,7 @@ _LINEAR_W4 = struct.Struct("@5i")
 class LinearW4:
     """sm_linear_w4: a Linear whose weights stay in 4 bits.  w [N, K / 2] uint8 (even k in the low four bits), scales [N, K / group]
     bf16, zeros [N, K / group] uint8 (None: 8), bias [N] bf16 or None.  The weights are packed here, once, into memory of the
-    object (a change of them afterwards needs a new object)."""
+    object (a change of them afterwards needs a new object); the bias stays the tensor given and is read by every call."""
 
     def __init__(self, w, scales, zeros=None, group=128, bias=None, stream=None):
         import torch

@@ -4,7 +4,7 @@
 // A lane has two 16-byte pieces of a head: below `rot` the two halves of its pairs, so that the rotation stays in the lane and an angle
 // serves both, behind it two adjacent pieces.  G lanes make a head, a wave takes 64 / G heads of one token at a time.
 // Angles: position times theta_i / 2 pi as a fraction of 2^64, modulo one revolution, is an integer product, which loses
-// nothing at far positions; its upper 32 bits go to the sine and cosine (bf16: the hardware's, whose 1e-6 is far below the rounding of the
+// nothing at far positions; its upper 32 bits go to the sine and cosine as a float, off by at most 2^-26 of a revolution (bf16: the hardware's, whose 1e-6 is far below the rounding of the
 // store; fp32: the library's, in units of pi).
 // Bound by the bytes read and written.
 #include "device_common.h"
@@ -160,9 +160,9 @@ __global__ __launch_bounds__(256) void head_norm_rope_kernel(HeadNormArgs a_) {
   }
 }
 
-// Few tokens: four waves share one (8 tokens of 32 + 8 + 8 heads of 128: 4.7 us instead of 7.9; 512 tokens: 7.3 instead of 9.3).  Once there is
-// a token for most of the 1024 SIMDs, one wave has all heads of a token and the angles are computed once (1024 tokens: 9.7 us instead of
-// 11.2; 16411: 82 instead of 121, 4.9 TB/s read and written, the rate of a large copy).
+// Few tokens: four waves share one (8 tokens of 32 + 8 + 8 heads of 128: 4.7 us instead of 7.9; 512 tokens: 7.3 instead of 9.5).  Once there is
+// a token for most of the 1024 SIMDs, one wave has all heads of a token and the angles are computed once (768 tokens: 9.6 us instead of 8.3;
+// 1024: 9.8 instead of 11.2; 16411: 81 instead of 122, 5.0 TB/s read and written).  Calls in a replayed graph.
 template <typename T, int G>
 static void launch_head_norm_g(HeadNormArgs& a, hipStream_t stream) {
   for (auto& p : a.part) p.units = (p.heads + 64 / G - 1) / (64 / G);

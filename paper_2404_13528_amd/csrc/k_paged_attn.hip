@@ -38,9 +38,10 @@ constexpr int PA_UNIT = 128;              // keys: chunks are whole units
 constexpr float PA_LOW = 0x1p-24f;
 
 // How the work is cut.  A chunk's start costs some 4 us (lengths, page table, first keys: three trips to memory), so at first there are as
-// many chunks as two workgroups a CU (heads over 128: one): 64 requests of 1000 keys take 54 us, with twice as many chunks 62.  But where
+// many chunks as two workgroups a CU (heads over 128: one): 64 requests of 1000 keys take 53 us, with twice as many chunks 59.  But where
 // that makes a chunk longer than 512 KB of keys and values, up to 4096 shorter ones balance the load better than they cost (64 requests of
-// 100 to 30000 keys: 271 us instead of 288).
+// 100 to 30000 keys, attention and join: 270 us instead of 313).  A table wider than its requests has more workgroups that end at once: one request
+// of 150 keys takes 7.4 us under a table of 160 tokens, 9.6 under one of 8192 and 10.2 under one of 131072.
 constexpr int PA_MANY_LOG2 = 12;
 struct PaShape {
   int rows, tiles, groups;                // query heads per tile, tiles per key head, workgroups per chunk
@@ -79,7 +80,9 @@ __device__ __forceinline__ unsigned pa_scan(unsigned x) {
 }
 
 // The chunk of workgroup `item`: request (-1: none), first key, one behind the last key, number of the request's chunks.
-// A lane has `per` requests.  With U units in all, `share` = U groups / 2^fill units would make 2^fill workgroups; every request has at least one
+// A lane has `per` requests.  Every workgroup reads all lengths, those past the fourth of a lane twice more: from some 500 requests on that takes longer
+// than the keys of short ones (requests of 100 keys with 32 heads over 8: 34 us for 256, 240 for 1024, 2300 for 4096).
+//  With U units in all, `share` = U groups / 2^fill units would make 2^fill workgroups; every request has at least one
 // chunk, so chunks of at least that length are at most 2^fill / groups + n_req.
 struct PaItem { int r, k0, k1, n; };
 __device__ __forceinline__ int pa_len(const PagedAttnArgs& a, int r) { return min(max(a.lens[r], 0), a.max_pages * a.page); }

@@ -9,6 +9,8 @@
 //    0x4300 in both halves is the pair of bf16 numbers 128 + w, exactly, in at most two instructions.
 //  * The products are integers times bf16 and the sums fp32.  What the offsets 128 + z add, (128 + z) sum of x, is taken off per
 //    group; the sum of x comes from the same instruction with ones as the second operand, so it has the layout of the result.
+//    The sums round relative to up to 143 |x| instead of |w - z| |x|, still far below the store's rounding (17 x 22016 x 4096: 432 of the
+//    374272 results are not the bf16 number nearest to the exact one, 215 of a plain fp32 computation).  From |x| = 2^113 on they overflow.
 //    Then the group's scale is applied, in fp32.  The rows of the result are the rows of x, a lane's column is one feature:
 //    it needs one word of scale and zero point per group.
 #include <algorithm>
@@ -124,8 +126,8 @@ __device__ __forceinline__ void w4_block(const w4_u32x4 wv, const unsigned (&sv)
 // waves' sums of a tile meet in LDS.
 // Loads return in the order of their issue, and the compiler's counting of them survives no branch: all loads are unconditional, and their
 // order is pinned.
-// On the GPU, weights cold: 1 x 4096 x 4096 (groups of 128) 4.0 us, 1 x 22016 x 4096 12.0 us (4.0 TB/s), 32 x 22016 x 4096 17.5 us,
-// 32 x 4096 x 11008 14.6 us.  Of 17 x 22016 x 4096's 16.6 us the stream of the weights alone takes 11, x 2, the products 3 and the end 1.
+// Calls in a replayed graph, groups of 128: 1 x 4096 x 4096 4.0 us, 1 x 22016 x 4096 11.7 us (4.1 TB/s), 32 x 22016 x 4096 18 us, 32 x 4096 x 11008
+// 15 us.  Of the 16 us of 17 x 22016 x 4096 in groups of 64 the stream of the weights alone takes 11; the rest is x, the products and the end.
 template <int MT, bool HALF, int NT, int GPB, int PB>
 __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
   __shared__ float red[W4_WAVES][NT][MT][16][17];
@@ -259,8 +261,8 @@ __global__ __launch_bounds__(64 * W4_WAVES, 2) void w4_kernel(W4Args p) {
 
 // Rows and tiles of a workgroup.  The time goes by the bytes that a CU takes in: a workgroup's rows of x (2 a k) and tiles of weights (8 and a
 // half a k, scales included), times the workgroups that a CU has; a tile's sums that meet at the end count like 6 more.  Measured against all
-// 15 choices at eleven sizes the one taken was within 0.4 us of the best: 32 x 4096 x 4096 takes 7.1 us with 16 rows and two tiles, 10.3 with
-// 32 and one; 32 x 11008 x 4096 12.9 us with 32 and three, 25 with 16 and one; 1 x 22016 x 4096 12.5 to 13.9 us.
+// 15 choices at twelve sizes the one taken was within 0.6 us of the best: 32 x 4096 x 4096 takes 7.1 us with 16 rows and two tiles, 10.3 with
+// 32 and one; 32 x 11008 x 4096 12.8 us with 32 and three, 25 with 16 and one; 1 x 22016 x 4096 11.5 to 13.3 us.
 struct W4Choice { int rows, nt; };
 static W4Choice w4_choose(int M, int tiles) {
   static const int NTS[5] = {1, 2, 3, 4, 6};
