@@ -896,6 +896,21 @@ class _Kept:
                 self.streams.add(raw)
         return raw
 
+    def __reduce__(self):                         # (a deep copy is of new memory, made on the current stream)
+        return _kept_again, (self.tensors,)
+
+
+def _kept_again(tensors):
+    return _Kept(tensors[0].device, None, *tensors)
+
+
+class _Keeper:
+    """An object with `_kept` memory.  Copying it uses the memory on the current stream."""
+
+    def __getstate__(self):
+        self._kept.used_on(self._kept.tensors[0].device, None)
+        return self.__dict__
+
 
 def _capturing(stream):
     import torch
@@ -1023,9 +1038,10 @@ class PagedAttentionDesc(C.Structure):
 
 
 _PAGED_ATTENTION = struct.Struct("@8ifq4q6q")             # PagedAttentionDesc in one step
+_in_turn = threading.Lock()
 
 
-class PagedAttention:
+class PagedAttention(_Keeper):
     """sm_paged_attention; owns its workspace.  q [n_req, heads_q, d], k_pages / v_pages [n_pages, page, heads_kv, d] (strided views: a
     head-major pool is passed permuted), table [n_req, max_pages] and lens [n_req] int32 -> o [n_req, heads_q, d]; lse: a contiguous
     fp32 [n_req, heads_q] to fill with the logarithm of the softmax sums.  Threads may share an object on one stream; calls on different
@@ -1037,7 +1053,7 @@ class PagedAttention:
             raise TypeError("unsupported dtype %s" % dtype)
         # (what stays the same from call to call; strides and pitch belong to a call, which packs a descriptor of its own)
         self.sizes = (SM_F32 if dtype == torch.float32 else SM_BF16, n_req, heads_q, heads_kv, d, page, max_pages, n_pages, d ** -0.5 if scale is None else scale)
-        self.dtype, self._one = dtype, threading.Lock()
+        self.dtype = dtype
         n = lib().sm_paged_attention_workspace_bytes(_PAGED_ATTENTION.pack(*self.sizes, max_pages, *[0] * 10))
         if n == 0:
             raise SmError("sm_paged_attention_workspace_bytes: " + lib().sm_last_error().decode())
@@ -1062,7 +1078,7 @@ class PagedAttention:
         raw = self._kept.used_on(dev, stream)
         if stream is not None:
             _lend(stream, q, k_pages, v_pages, table, lens, out, lse)
-        with self._one:                           # (a call's two kernels follow each other in the stream)
+        with _in_turn:                            # (a call's two kernels follow each other in the stream)
             check(lib().sm_paged_attention(desc, *args, self.ws.numel(), raw), "sm_paged_attention")
         return out
 
@@ -1074,7 +1090,7 @@ class LinearW4Desc(C.Structure):
 _LINEAR_W4 = struct.Struct("@5i")
 
 
-class LinearW4:
+class LinearW4(_Keeper):
     """sm_linear_w4: a Linear whose weights stay in 4 bits.  w [N, K / 2] uint8 (even k in the low four bits), scales [N, K / group]
     bf16, zeros [N, K / group] uint8 (None: 8), bias [N] bf16 or None.  The weights are packed here, once, into memory of the
     object (a change of them afterwards needs a new object); the bias stays the tensor given and is read by every call."""

@@ -9,6 +9,7 @@ fp32 (the library's), times the pair.
 Attention: a logit's error is below (d + 4) 2^-24 of sum |q k| * |scale| (products exact in bf16, sums in fp32), and moves a weight by
 that much, numerator and denominator; the weights themselves carry 2^-16 (bf16: two terms of 8 bits each) resp. 2^-22, and sums of up
 to n keys in blocks (n / 16 + 64) 2^-24 of sum p |v|."""
+import copy
 import threading
 
 import numpy as np
@@ -848,6 +849,24 @@ def test_objects_made_on_a_busy_stream_and_called_on_another(name, given):
 
 
 @pytest.mark.parametrize("name", ["attention", "linear"])
+def test_copies_of_objects(name):
+    """A shallow copy shares the memory, a deep one has its own."""
+    make, call, memory = attention_and_linear()[name]
+    o = make()
+    want = call(o).clone()
+    shallow, deep = copy.copy(o), copy.deepcopy(o)
+    assert memory(shallow).data_ptr() == memory(o).data_ptr() != memory(deep).data_ptr()
+    memory(o).fill_(0xff) if name == "attention" else None
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for c in (shallow, deep):
+        assert torch.equal(call(c), want)
+        got = call(c, stream=side)
+        side.synchronize()
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("name", ["attention", "linear"])
 @pytest.mark.parametrize("given", [True, False])
 def test_objects_that_go_while_another_stream_uses_them(name, given):
     """Their memory is not handed out before that stream is done."""
@@ -891,6 +910,53 @@ def test_weights_dropped_while_another_stream_packs_them():
         apart = not at & {t.data_ptr() for t in new}
         torch.cuda.synchronize()
         assert apart and torch.equal(lin.packed, want)
+
+
+def test_copy_of_a_linear_that_another_stream_is_packing():
+    g = torch.Generator().manual_seed(21)
+    w, sc = torch.randint(0, 256, (4096, 1024), generator=g, dtype=torch.uint8).cuda(), torch.rand(4096, 16, generator=g).to(BF16).cuda()
+    want = sm.LinearW4(w, sc).packed.clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        busy(1 << 20)
+    lin = sm.LinearW4(w, sc, stream=side)
+    again = copy.deepcopy(lin)
+    del lin
+    torch.cuda.synchronize()
+    assert torch.equal(again.packed, want)
+
+
+def test_captured_with_the_stream_given():
+    """Every call names the stream that is being captured, and makes or is given its results."""
+    g = torch.Generator().manual_seed(22)
+    x = torch.randn(20, 8, 64, generator=g).to(BF16).cuda()
+    gain, pos = torch.ones(64, dtype=BF16, device="cuda"), torch.arange(20, dtype=I32, device="cuda")
+    kp, vp = torch.randn(2, 20, 16, 2, 64, generator=g).to(BF16).cuda()
+    table, lens = torch.arange(20, dtype=I32, device="cuda").view(10, 2).repeat(2, 1), torch.zeros(20, dtype=I32, device="cuda")
+    lin = sm.LinearW4(torch.randint(0, 256, (40, 128), generator=g, dtype=torch.uint8).cuda(), torch.rand(40, 2, generator=g).to(BF16).cuda())
+    att, eager = (sm.PagedAttention(20, 4, 2, 64, 16, 2, 20, BF16) for _ in range(2))
+    one, free, n_free, pages = ints([1] * 20), ints(range(40)), ints([40]), torch.full((20, 3), -1, dtype=I32, device="cuda")
+    y = torch.empty(20, 40, dtype=BF16, device="cuda")
+
+    def calls(a, s, out):
+        q = sm.head_norm_rope(x[:, :4], None, None, pos, q_gamma=gain, stream=s)[0]
+        o = a(q, kp, vp, table, lens, stream=s)
+        lin(o.view(20, 256), out=out, stream=s)
+        return (q, o, out) + tuple(sm.page_table(lens, one, free, n_free, pages, 16, 40, 20, stream=s))
+    calls(att, None, y)
+    torch.cuda.synchronize()
+    cg = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(cg):
+        got = calls(att, torch.cuda.current_stream(), y)
+    for i in range(3):
+        x.copy_(torch.randn(20, 8, 64, generator=g).to(BF16))
+        lens.copy_(torch.randint(0, 33, (20,), generator=g))
+        cg.replay()
+        torch.cuda.synchronize()
+        want = calls(eager, None, torch.empty_like(y))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_binding_refuses_wrong_tensors():
