@@ -493,8 +493,8 @@ int sm_head_norm_rope(const sm_head_norm_rope_desc*, const void* q, const void* 
  * multiple of heads_kv).  No token (lens[r] <= 0, or no page of them exists), or none with a logit above -inf: o = 0,
  * lse = -inf.  A NaN among the logits: NaN.  lse (nullable) [n_req, heads_q] fp32, contiguous: the natural logarithm of
  * the sum of exp(scale * q . k), with which results over disjoint parts of a cache can be joined.  What lies in a page
- * behind the request's last token is not used, whatever it is; finite values are taken at any size, and one of a key that
- * weighs nothing adds nothing.  o must not overlap the inputs.  Strides: request, head (q, o); page, token, head (k_pages,
+ * behind the request's last token is not used, whatever it is; finite values are taken at any size (2^20 of the largest
+ * together; the smallest result is 2^-129), and one of a key that weighs nothing adds nothing.  o must not overlap the inputs.  Strides: request, head (q, o); page, token, head (k_pages,
  * v_pages: token-major [page, token, head, d] and head-major [page, head, token, d] pools alike; page and token strides not
  * negative, a pool's pages within 64 GiB).  The key axis is split over workgroups by the lengths found on the device and
  * joined in fp32.

@@ -33,9 +33,10 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 pa_bf16x8;
 
 constexpr int PA_ROWS = 16;               // query heads a workgroup serves at once
 constexpr int PA_UNIT = 128;              // keys: chunks are whole units
-// The weights go to their product with the values as multiples of this, so that a sum of 2^24 values of any finite size is finite.  Every wave and
-// chunk sums by its own maximum: without it large values of keys that weigh nothing beside another chunk's would be infinite there.
-constexpr float PA_LOW = 0x1p-24f;
+// The weights go to their product with the values as multiples of this, so that a sum of 2^20 values of any finite size is finite.  Every wave and
+// chunk sums by its own maximum: without it large values of keys that weigh nothing beside another chunk's would be infinite there.  The
+// smallest number a sum can hold becomes 2^-129, an eighth of the smallest normal one.
+constexpr float PA_LOW = 0x1p-20f;
 
 // How the work is cut.  A chunk's start costs some 4 us (lengths, page table, first keys: three trips to memory), so at first there are as
 // many chunks as two workgroups a CU (heads over 128: one): 64 requests of 1000 keys take 53 us, with twice as many chunks 59.  But where
@@ -277,7 +278,7 @@ __device__ __forceinline__ void pa_values(PaTile<T, DP>& t, float* s, const unsi
 #pragma unroll
   for (int i = 0; i < NV; ++i) { p[i] = __builtin_amdgcn_exp2f(s[i] - ref); l += p[i]; }
   if constexpr (sizeof(T) == 2) {
-    // A term is the upper 8 bits of what is left of the weight.  All three are above zero wherever the weight is (down to 2^-63), so that an infinite
+    // A term is the upper 8 bits of what is left of the weight.  All three are above zero wherever the weight is (down to 2^-67), so that an infinite
     // value keeps its sign: 0 x inf is no number.  That takes a factor of 1 + 2^-23 on all weights alike and one of 1 + 2^-16 on the part below
     // 2^-7 of one, so a weight is off by at most 2^-22.  (With a step more per term two registers spill: 64 requests of 100 to 30000 keys take
     // 282 us instead of 270, as with two terms.)

@@ -458,6 +458,22 @@ def test_paged_attention_values_whose_sum_is_no_float(n, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("low", [-60, -100, -115, -126])
+def test_paged_attention_smallest_values(low, dtype):
+    """Values around 2^low: on top of the usual rounding a sum's steps are no finer than 2^-129, as are those of a bf16 result below 2^-126 (2^-133)."""
+    g = torch.Generator().manual_seed(-low)
+    n, d = 500, 64
+    kp, vp = torch.randn(32, 16, 1, d, generator=g).to(dtype), (torch.randn(32, 16, 1, d, generator=g).double() * 2.0 ** low).to(dtype)
+    q = torch.randn(1, 4, d, generator=g).to(dtype)
+    ids = torch.randperm(32, generator=g)[None]
+    o, lse, av, aw = P.paged_attention(to_np(q), to_np(kp), to_np(vp), ids.numpy(), [n], 0.125, want_bound=True)
+    got = sm.PagedAttention(1, 4, 1, d, 16, 32, 32, dtype, scale=0.125)(q.cuda(), kp.cuda(), vp.cuda(), ids.to(I32).cuda(), ints([n]))
+    score = (d + 4) * 2.0 ** -24 * aw + (np.abs(lse)[..., None] + 4) * 2.0 ** -23
+    tol = HALF[dtype] * np.abs(o) + (2 * score + 2.0 ** -22 + (n / 16 + 64) * 2.0 ** -24) * av + (n / 16 + 64) * 2.0 ** -130 + 2.0 ** -134
+    check(got, o, tol, "o")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_paged_attention_weights_carry_fp32(d, dtype):
     """Two keys with values 1 and -1 and logits 0 and -x: the result is tanh(x / 2), a difference of weights near 1 that shows what each of
